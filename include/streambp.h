@@ -350,6 +350,80 @@ int32_t streambp_stack_backward(const sbp_stack_cfg *cfg, const sbp_layer_weight
                                 float *demb, void *dx0, float *loss, int64_t *n_active,
                                 void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* -------------------------------------------------------- optimizer step -- */
+
+/* What follows a backward: the norm of all gradients, and one AdamW step (decoupled weight decay) over many tensors, large
+ * and small, in few launches.  With t = step and g = *grad_scale * grad (1 without grad_scale), for every element
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32 (what depends on the hyperparameters alone in fp64).  p is `master` where there is one, else param.
+ *
+ * A bf16 param with a master copy is the copy rounded to nearest.  Without one it is rounded stochastically, up with the probability of
+ * what is cut off: an update of less than half a step of the weight would never arrive otherwise.
+ *
+ * SBP_STATE_8BIT keeps m and sqrt(v) as e4m3 values (OCP FP8, 1 byte per element) with a power of two per SBP_STATE_BLOCK
+ * consecutive elements (OCP E8M0, 1 byte: 2^(byte - 127)), 2.008 instead of 8 bytes per element: value = e4m3 * 2^(byte - 127), the
+ * block's largest magnitude lies in [128, 256) of it (down to 2^-126; a block of zeros has byte 1).  All zeros is a valid start.  Stored
+ * stochastically too: sqrt(v) changes by less than a rounding step at a time.  sqrt(v) > 0 is never stored as zero: an element whose v vanished
+ * would take a step of m / eps.  What is not finite is stored as NaN and does not count for the block's power of two.  The step itself uses
+ * m and v before they are rounded.
+ *
+ * Random bits: of element i (its low 32 bits) of the k-th tensor of the call
+ *   r = mix(i ^ key), key = mix(mix(mix(seed) + step) + k), 32-bit arithmetic (for i >= 2^32: key = mix(key + (i >> 32)))
+ *   mix(x): x = (x ^ x >> 16) * 0x9E3779B1;  x = (x ^ x >> 15) * 0xB504F333;  x ^ x >> 16
+ * a bf16 param adds r & 0xffff below its last bit, m (r >> 12) / 2^20 and sqrt(v) (r & 0xfffff) / 2^20 of a step, and cut off.  The same call
+ * gives the same bits every time. */
+enum { SBP_STATE_F32 = 0, SBP_STATE_8BIT = 1 };
+enum { SBP_STATE_BLOCK = 256 };
+
+typedef struct {
+  int32_t state;        /* SBP_STATE_F32 or SBP_STATE_8BIT                            */
+  int32_t step;         /* t >= 1, this step's number                                 */
+  double lr, beta1, beta2, eps;  /* lr >= 0 and finite; 0 <= beta1, beta2 < 1; eps >= 0 */
+  uint32_t seed;        /* of the random bits                                         */
+  int32_t zero_grads;   /* 1: the gradients become zero after they are read, as "+=" accumulators have to
+                           before the next backward                                  */
+} sbp_adamw_cfg;
+
+/* One tensor: n >= 0 elements, dense, in any order that its parts share (n = 0: the pointers are not read).  Tensors of a call
+ * may not overlap.  Pointers need the alignment of their elements; where param, master, grad, m and v are 16-byte aligned (8-bit m, v: 8) the
+ * step is as fast as memory, otherwise several times slower. */
+typedef struct {
+  int64_t n;
+  int32_t dtype;        /* of param: SBP_F32 or SBP_BF16                              */
+  int32_t grad_dtype;   /* of grad: SBP_F32 or SBP_BF16                               */
+  double weight_decay;  /* >= 0 and finite; usually 0 for norm gains                  */
+  void *param;          /* in / out (with a master copy: out)                         */
+  float *master;        /* fp32 copy of a bf16 param, in / out, or NULL               */
+  void *grad;           /* in (zero_grads: in / out)                                  */
+  void *m, *v;          /* in / out: SBP_STATE_F32 fp32 m and v; SBP_STATE_8BIT e4m3 m and sqrt(v) */
+  void *m_scale, *v_scale;  /* in / out, SBP_STATE_8BIT: ceil(n / SBP_STATE_BLOCK) bytes each; NULL otherwise */
+} sbp_adamw_tensor;
+
+/* Device memory: what changes from one replay of a captured step to the next */
+typedef struct {
+  double lr;
+  int32_t step;
+  int32_t pad;
+} sbp_adamw_now;
+
+/*   tensors     HOST array, read before the call returns
+ *   grad_scale  DEVICE fp32 scalar or NULL.  If it is not finite, params, states and master copies stay as they are (gradients
+ *               still become zero if zero_grads is set)
+ *   now         DEVICE or NULL: step and lr are read from it when the step runs, in place of cfg's (which are not
+ *               looked at); a step < 1 there is taken as 1 */
+int32_t streambp_adamw_step(const sbp_adamw_cfg *cfg, int32_t n_tensors, const sbp_adamw_tensor *tensors,
+                            const float *grad_scale, const sbp_adamw_now *now, void *hip_stream);
+
+/* The norm of all gradients of the same table (only n, grad and grad_dtype are looked at), and the factor that limits it:
+ *   norm [1] fp32 out = sqrt(sum of squares);   grad_scale [1] fp32 out (or NULL) = min(1, max_norm / norm), 1 for max_norm = 0 (no limit)
+ *   or norm 0, NaN where the norm is not finite, which makes streambp_adamw_step leave everything as it was.
+ * Squares and sums of eight are fp32, what they add up to fp64, in a fixed order: an element of 1.8e19 or more counts as
+ * not finite.  workspace: streambp_grad_norm_workspace_bytes(n_tensors) bytes. */
+size_t streambp_grad_norm_workspace_bytes(int32_t n_tensors);
+int32_t streambp_grad_norm(int32_t n_tensors, const sbp_adamw_tensor *tensors, float max_norm, float *norm,
+                           float *grad_scale, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* ------------------------------------------------------------------ misc -- */
 
 const char *streambp_version(void);

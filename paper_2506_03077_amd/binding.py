@@ -15,6 +15,8 @@ LIB_PATH = os.environ.get("STREAMBP_LIB") or os.path.join(_PKG, "libstreambp.so"
 
 SBP_F32, SBP_BF16 = 0, 1
 SBP_OBJ_SFT, SBP_OBJ_GRPO, SBP_OBJ_DPO = 0, 1, 2
+SBP_STATE_F32, SBP_STATE_8BIT = 0, 1
+SBP_STATE_BLOCK = 256
 WEIGHT_NAMES = ("wq", "wk", "wv", "wo", "wgate", "wup", "wdown", "g1", "g2")
 
 
@@ -67,6 +69,16 @@ class StackCfg(C.Structure):
     _fields_ = [("layer", LayerCfg), ("n_layers", C.c_int32), ("vocab", C.c_int32), ("head_chunk", C.c_int32),
                 ("objective", C.c_int32), ("loss_scale", C.c_float), ("clip_eps", C.c_float), ("kl_beta", C.c_float),
                 ("kl_mode", C.c_int32), ("final_eps", C.c_float)]
+
+
+class AdamwCfg(C.Structure):
+    _fields_ = [("state", C.c_int32), ("step", C.c_int32), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("seed", C.c_uint32), ("zero_grads", C.c_int32)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("weight_decay", C.c_double)] + \
+        [(n, C.c_void_p) for n in ("param", "master", "grad", "m", "v", "m_scale", "v_scale")]
 
 
 _lib = None
@@ -160,6 +172,12 @@ def lib():
                                                      vp, vp, vp, vp, vp]
         L.streambp_debug_mfma_rate.restype = C.c_int
         L.streambp_debug_mfma_rate.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, vp]
+        L.streambp_adamw_step.restype = i32
+        L.streambp_adamw_step.argtypes = [C.POINTER(AdamwCfg), i32, C.POINTER(AdamwTensor), vp, vp, vp]
+        L.streambp_grad_norm_workspace_bytes.restype = sz
+        L.streambp_grad_norm_workspace_bytes.argtypes = [i32]
+        L.streambp_grad_norm.restype = i32
+        L.streambp_grad_norm.argtypes = [i32, C.POINTER(AdamwTensor), f32, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -417,6 +435,76 @@ def streambp_embedding_backward(ids, dx, vocab, demb=None, stream=None):
         demb = torch.zeros((vocab, d), dtype=torch.float32, device=dx.device)
     _check(lib().streambp_embedding_backward(_dt_code(dx), ids.numel(), d, vocab, _ptr(ids), _ptr(dx), _ptr(demb), _stream(stream)))
     return demb
+
+
+def adamw_cfg(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, state=SBP_STATE_F32, seed=0, zero_grads=False):
+    return AdamwCfg(int(state), int(step), lr, beta1, beta2, eps, int(seed), int(zero_grads))
+
+
+def adamw_tensors(tensors):
+    """The table of tensors of streambp_adamw_step and streambp_grad_norm, made once: a list of dicts of device tensors param, grad, m, v
+    (for the norm grad alone), where they belong master, m_scale, v_scale, and weight_decay (0).  It holds the tensors."""
+    table = (AdamwTensor * len(tensors))()
+    table.tensors = [dict(t) for t in tensors]
+    for x, t in zip(table, table.tensors):
+        decay = t.pop("weight_decay", 0.0)
+        unknown = set(t) - {"param", "master", "grad", "m", "v", "m_scale", "v_scale"}
+        assert not unknown, f"unknown entries {sorted(unknown)}"
+        n = t["grad"].numel()
+        for name in ("param", "master", "m", "v"):
+            assert t.get(name) is None or t[name].numel() == n, f"{name} and grad must have the same number of elements"
+        for name in ("m_scale", "v_scale"):
+            assert t.get(name) is None or t[name].numel() == -(-n // SBP_STATE_BLOCK) and t[name].element_size() == 1, f"{name}: a byte per {SBP_STATE_BLOCK} elements"
+        size = 4 if t.get("m_scale") is None else 1
+        assert all(t.get(name) is None or t[name].element_size() == size for name in ("m", "v")), "m and v: fp32, or bytes with m_scale and v_scale"
+        x.n, x.grad_dtype, x.weight_decay = n, _dt_code(t["grad"]), decay
+        if t.get("param") is not None:
+            x.dtype = _dt_code(t["param"])
+        assert t.get("master") is None or _dt_code(t["master"]) == SBP_F32, "master must be fp32"
+        for name, y in t.items():
+            setattr(x, name, _ptr(y))
+    return table
+
+
+def new_adamw_states(param, state=SBP_STATE_F32, master=False):
+    """The entries of a tensor of adamw_tensors that a program keeps beside `param` and its gradient, before the first step."""
+    torch = _torch()
+    new = lambda n, dtype: torch.zeros(n, dtype=torch.uint8 if dtype != torch.float32 else dtype, device=param.device).view(dtype)
+    n, blocks = param.numel(), -(-param.numel() // SBP_STATE_BLOCK)
+    out = dict(param=param)
+    if int(state) == SBP_STATE_8BIT:
+        out.update(m=new(n, torch.float8_e4m3fn), v=new(n, torch.float8_e4m3fn), m_scale=new(blocks, torch.float8_e8m0fnu), v_scale=new(blocks, torch.float8_e8m0fnu))
+    else:
+        out.update(m=new(n, torch.float32), v=new(n, torch.float32))
+    if master:
+        out["master"] = param.float()
+    return out
+
+
+def streambp_adamw_step(cfg: AdamwCfg, tensors, grad_scale=None, now=None, stream=None):
+    """One step over the tensors of adamw_tensors(...), in place.  grad_scale: 1-element fp32 device tensor; now: device memory that holds a
+    sbp_adamw_now (16 bytes: lr as fp64, step as int32), for captured steps."""
+    torch = _torch()
+    assert grad_scale is None or grad_scale.dtype == torch.float32
+    assert now is None or now.numel() * now.element_size() >= 16
+    _check(lib().streambp_adamw_step(C.byref(cfg), len(tensors), tensors, _ptr(grad_scale), _ptr(now), _stream(stream)))
+
+
+def streambp_grad_norm_workspace_bytes(n_tensors) -> int:
+    return int(lib().streambp_grad_norm_workspace_bytes(n_tensors))
+
+
+def streambp_grad_norm(tensors, max_norm=0.0, norm=None, grad_scale=None, workspace=None, stream=None):
+    """Returns (norm, grad_scale), 1-element fp32 device tensors; max_norm 0: no limit."""
+    torch = _torch()
+    if norm is None or grad_scale is None or workspace is None:
+        dev = next((t["grad"].device for t in tensors.tensors), torch.device("cuda", torch.cuda.current_device()))
+        norm = torch.empty(1, dtype=torch.float32, device=dev) if norm is None else norm
+        grad_scale = torch.empty(1, dtype=torch.float32, device=dev) if grad_scale is None else grad_scale
+        workspace = _workspace(streambp_grad_norm_workspace_bytes(len(tensors)), dev) if workspace is None else workspace
+    assert norm.dtype == grad_scale.dtype == torch.float32
+    _check(lib().streambp_grad_norm(len(tensors), tensors, float(max_norm), _ptr(norm), _ptr(grad_scale), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return norm, grad_scale
 
 
 def streambp_layer_fast_path(cfg: LayerCfg) -> int:

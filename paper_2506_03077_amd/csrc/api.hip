@@ -16,17 +16,17 @@
 
 using namespace sbp;
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-int32_t fail(int32_t code, const char* fmt, ...) {
+int32_t sbp::fail(int32_t code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return code;
 }
+
+namespace {
 
 #define HIPCHK(expr)                                                                       \
   do {                                                                                     \

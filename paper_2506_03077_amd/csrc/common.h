@@ -9,6 +9,9 @@ namespace sbp {
 
 enum DType : int { DT_F32 = 0, DT_BF16 = 1 };
 
+// The message of streambp_last_error() (printf form); returns `code`
+int32_t fail(int32_t code, const char* fmt, ...);
+
 inline size_t dtype_size(int dt) { return dt == DT_BF16 ? 2 : 4; }
 
 static inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -1,0 +1,336 @@
+// Optimizer step for gfx950: AdamW over a table of tensors, and the norm of their gradients.
+//
+// Both stream memory once: per element AdamW reads weight, gradient and two states and writes weight and states back, and does some fifty vector
+// instructions.  A thread has eight consecutive elements, in 16-byte loads; 32 threads have a block of 256, whose magnitudes meet
+// in registers where the states have 8 bits.
+#include "optim.h"
+#include "device.h"
+
+namespace sbp {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int THREADS = 256, PER = 8, TILE = THREADS * PER;      // elements of a thread, of a pass of the workgroup
+
+struct AdamwTable { AdamwArgs a; int n; AdamwTensor t[ADAMW_TABLE]; };
+struct NormTable { double* part; int64_t span; int n; NormTensor t[NORM_TABLE]; };
+static_assert(sizeof(AdamwTable) <= 4096 && sizeof(NormTable) <= 4096, "arguments of a launch");
+
+// The tensor of a workgroup: the last one that begins at or before it
+template <typename Table>
+__device__ __forceinline__ int tensor_of(const Table& table, uint32_t group) {
+  int lo = 0, hi = table.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (table.t[mid].first_group <= group) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// ---- eight elements ---------------------------------------------------------------------------------------------
+// WHOLE: all eight exist and their address is a multiple of 16 (bytes: 8); else `n` of them, element by element.
+__device__ __forceinline__ void load8(float (&x)[8], const float* p) {
+  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+}
+__device__ __forceinline__ void load8(float (&x)[8], const bf16_t* p) {
+  const u32x4 a = *(const u32x4*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(a[i] << 16); x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
+  *(f32x4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {      // to nearest
+  bf16x8 a;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = (bf16_t)x[i];
+  *(bf16x8*)p = a;
+}
+template <bool WHOLE, typename T> __device__ __forceinline__ void get(float (&x)[8], const T* p, int n) {
+  if constexpr (WHOLE) { load8(x, p); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = i < n ? ldf(p + i) : 0.f;
+}
+template <bool WHOLE, typename T> __device__ __forceinline__ void put(T* p, const float (&x)[8], int n) {
+  if constexpr (WHOLE) { store8(p, x); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) stf(p + i, x[i]);
+}
+template <bool WHOLE> __device__ __forceinline__ u32x2 get_bytes(const uint8_t* p, int n) {
+  if constexpr (WHOLE) return *(const u32x2*)p;
+  u32x2 w = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+  return w;
+}
+template <bool WHOLE> __device__ __forceinline__ void put_bytes(uint8_t* p, const u32x2& w, int n) {
+  if constexpr (WHOLE) { *(u32x2*)p = w; return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+}
+
+// ---- random bits: see the public header
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x9E3779B1u;
+  x = (x ^ (x >> 15)) * 0xB504F333u;
+  return x ^ (x >> 16);
+}
+
+// ---- e4m3 times a power of two ----------------------------------------------------------------------------------
+// Largest bit pattern of non-negative floats over the 32 lanes that share a block: the order of the patterns is that of the values, NaN above infinity.
+__device__ __forceinline__ uint32_t max_of_block(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true));       // lane ^ 1
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true));       // lane ^ 2
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true));      // mirrored within 8 lanes
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, true));      // ... within 16
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x, x, false, false));
+  return max(r[0], r[1]);
+}
+constexpr uint32_t NOT_FINITE = 0x7f800000u;
+// The byte of a block whose largest magnitude has this pattern: 2^(byte - 127) brings it to [128, 256)
+__device__ __forceinline__ uint32_t scale_byte(uint32_t largest) { return max(largest >> 23, 8u) - 7u; }
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(max(byte << 23, 0x00400000u)); }      // (byte 0: 2^-127, below the normal range)
+__device__ __forceinline__ float inverse_scale_of(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }       // byte 1 .. 248
+// x * inverse as the code of an e4m3 value, u / 2^20 of a step added before the rest is cut off: a float 2^120 times smaller has the e4m3 value's
+// exponent, and below its smallest normal one its fixed point, twenty bits further up.
+__device__ __forceinline__ uint32_t e4m3_code(float x, float inverse, uint32_t u) {
+  const uint32_t b = __float_as_uint(fabsf(x) * inverse * 0x1p-120f);
+  return min((b + u) >> 20, 0x7fu);      // (infinities and NaN: NaN)
+}
+
+struct Consts { float beta1, rest1, beta2, rest2, eps, bias1, bias2; double lr; uint32_t key; float grad_scale; };
+
+template <bool WHOLE, typename P, bool MASTER, typename G, bool EIGHT>
+__device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Consts& c, float keep, int64_t e, int n, bool zero) {
+  float g[8], w[8], m[8], v[8];
+  if constexpr (MASTER) get<WHOLE>(w, t.master + e, n); else get<WHOLE>(w, (const P*)t.param + e, n);
+  get<WHOLE>(g, (const G*)t.grad + e, n);
+  if constexpr (EIGHT) {
+    const u32x2 mb = get_bytes<WHOLE>((const uint8_t*)t.m + e, n), vb = get_bytes<WHOLE>((const uint8_t*)t.v + e, n);
+    const bool in = WHOLE || n > 0;
+    const float ms = in ? scale_of(t.m_scale[e / ADAMW_BLOCK]) : 0.f, vs = in ? scale_of(t.v_scale[e / ADAMW_BLOCK]) : 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f32x2 m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mb[i], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mb[i], true);
+      const f32x2 v0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vb[i], false), v1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vb[i], true);
+      m[4 * i] = m0[0] * ms; m[4 * i + 1] = m0[1] * ms; m[4 * i + 2] = m1[0] * ms; m[4 * i + 3] = m1[1] * ms;
+      v[4 * i] = v0[0] * vs; v[4 * i + 1] = v0[1] * vs; v[4 * i + 2] = v1[0] * vs; v[4 * i + 3] = v1[1] * vs;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= v[i];
+  } else {
+    get<WHOLE>(m, (const float*)t.m + e, n);
+    get<WHOLE>(v, (const float*)t.v + e, n);
+  }
+  float root[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = g[i] * c.grad_scale;
+    m[i] = m[i] * c.beta1 + x * c.rest1;
+    v[i] = v[i] * c.beta2 + x * x * c.rest2;
+    root[i] = sqrtf(v[i]);
+    w[i] = w[i] * keep - c.bias1 * m[i] / (root[i] * c.bias2 + c.eps);
+  }
+  uint32_t r[8];
+  constexpr bool ROUNDS = sizeof(P) == 2 && !MASTER;
+  if constexpr (EIGHT || ROUNDS) {
+    const uint32_t key = e >> 32 ? mix(c.key + (uint32_t)(e >> 32)) : c.key;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = mix((uint32_t)(e + i) ^ key);
+  }
+  if constexpr (EIGHT) {
+    uint32_t mx = 0, vx = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (WHOLE || i < n) { mx = max(mx, __float_as_uint(m[i]) & 0x7fffffffu); vx = max(vx, __float_as_uint(root[i]) & 0x7fffffffu); }
+    mx = max_of_block(mx);
+    vx = max_of_block(vx);
+    if (__builtin_amdgcn_ballot_w64(max(mx, vx) >= NOT_FINITE) != 0) {      // they become NaN, and the scale is that of the others
+      mx = vx = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t x = __float_as_uint(m[i]) & 0x7fffffffu, y = __float_as_uint(root[i]) & 0x7fffffffu;
+        if ((WHOLE || i < n) && x < NOT_FINITE) mx = max(mx, x);
+        if ((WHOLE || i < n) && y < NOT_FINITE) vx = max(vx, y);
+      }
+      mx = max_of_block(mx);
+      vx = max_of_block(vx);
+    }
+    const uint32_t mb = scale_byte(mx), vb = scale_byte(vx);
+    const float mi = inverse_scale_of(mb), vi = inverse_scale_of(vb);
+    u32x2 mc = {0, 0}, vc = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      mc[i >> 2] |= (e4m3_code(m[i], mi, r[i] >> 12) | (__float_as_uint(m[i]) >> 24 & 0x80u)) << (8 * (i & 3));
+      vc[i >> 2] |= max(e4m3_code(root[i], vi, r[i] & 0xfffffu), root[i] > 0.f ? 1u : 0u) << (8 * (i & 3));
+    }
+    put_bytes<WHOLE>((uint8_t*)t.m + e, mc, n);
+    put_bytes<WHOLE>((uint8_t*)t.v + e, vc, n);
+    if ((threadIdx.x & 31) == 0 && (WHOLE || n > 0)) { t.m_scale[e / ADAMW_BLOCK] = (uint8_t)mb; t.v_scale[e / ADAMW_BLOCK] = (uint8_t)vb; }
+  } else {
+    put<WHOLE>((float*)t.m + e, m, n);
+    put<WHOLE>((float*)t.v + e, v, n);
+  }
+  if constexpr (MASTER) put<WHOLE>(t.master + e, w, n);
+  if constexpr (ROUNDS) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t b = __float_as_uint(w[i]);
+      w[i] = __uint_as_float((b & NOT_FINITE) == NOT_FINITE ? b : (b + (r[i] & 0xffffu)) & 0xffff0000u);      // (then exact; infinities and NaN as they are)
+    }
+  }
+  put<WHOLE>((P*)t.param + e, w, n);
+  if (zero) {
+    const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    put<WHOLE>((G*)t.grad + e, none, n);
+  }
+}
+
+template <typename P, bool MASTER, typename G, bool EIGHT>
+__device__ __forceinline__ void span_of(const AdamwTensor& t, const Consts& c, int64_t first, bool zero) {
+  auto whole16 = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
+  auto whole8 = [](const void* p) { return ((uintptr_t)p & 7) == 0; };
+  const bool aligned = whole16(t.param) && whole16(t.master) && whole16(t.grad) && (EIGHT ? whole8(t.m) && whole8(t.v) : whole16(t.m) && whole16(t.v));
+  const float keep = (float)(1.0 - c.lr * t.weight_decay);
+  const int64_t end = min(first + ADAMW_SPAN, t.n);
+  for (int64_t at = first; at < end; at += TILE) {
+    const int64_t e = at + threadIdx.x * PER;
+    if (aligned && at + TILE <= t.n) eight_elements<true, P, MASTER, G, EIGHT>(t, c, keep, e, PER, zero);
+    else eight_elements<false, P, MASTER, G, EIGHT>(t, c, keep, e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)), zero);
+  }
+}
+
+template <bool EIGHT>
+__global__ __launch_bounds__(THREADS) void adamw_k(const AdamwTable table) {
+  const AdamwArgs& a = table.a;
+  const AdamwTensor& t = table.t[tensor_of(table, blockIdx.x)];
+  const int64_t first = (int64_t)(blockIdx.x - t.first_group) * ADAMW_SPAN;
+  Consts c;
+  c.beta1 = (float)a.beta1; c.rest1 = (float)(1.0 - a.beta1); c.beta2 = (float)a.beta2; c.rest2 = (float)(1.0 - a.beta2);
+  c.eps = (float)a.eps; c.bias1 = a.bias1; c.bias2 = a.bias2; c.lr = a.lr;
+  c.grad_scale = a.grad_scale ? *a.grad_scale : 1.f;
+  int step = a.step;
+  if (a.now) {
+    step = max(1, a.now->step);
+    c.lr = a.now->lr;
+    c.bias1 = (float)(c.lr / (a.beta1 > 0.0 ? -expm1(step * log(a.beta1)) : 1.0));
+    c.bias2 = (float)(1.0 / sqrt(a.beta2 > 0.0 ? -expm1(step * log(a.beta2)) : 1.0));
+  }
+  c.key = mix(mix(mix(a.seed) + (uint32_t)step) + t.index);
+  const bool zero = a.zero_grads != 0;
+  if (!(fabsf(c.grad_scale) < INFINITY)) {      // nothing is known of the gradients: nothing moves
+    if (!zero) return;
+    const int64_t end = min(first + ADAMW_SPAN, t.n);
+    for (int64_t e = first + threadIdx.x; e < end; e += THREADS) {
+      if (t.grad_dtype == DT_BF16) stf((bf16_t*)t.grad + e, 0.f); else stf((float*)t.grad + e, 0.f);
+    }
+    return;
+  }
+  const bool gb = t.grad_dtype == DT_BF16;
+  if (t.dtype == DT_F32) { if (gb) span_of<float, false, bf16_t, EIGHT>(t, c, first, zero); else span_of<float, false, float, EIGHT>(t, c, first, zero); }
+  else if (t.master) { if (gb) span_of<bf16_t, true, bf16_t, EIGHT>(t, c, first, zero); else span_of<bf16_t, true, float, EIGHT>(t, c, first, zero); }
+  else { if (gb) span_of<bf16_t, false, bf16_t, EIGHT>(t, c, first, zero); else span_of<bf16_t, false, float, EIGHT>(t, c, first, zero); }
+}
+
+hipError_t adamw_step(const AdamwArgs& a, const AdamwTensor* t, int n, hipStream_t st) {
+  if (n < 1 || n > ADAMW_TABLE) return hipErrorInvalidValue;
+  AdamwTable table{};
+  table.a = a;
+  table.n = n;
+  int64_t groups = 0;
+  for (int i = 0; i < n; ++i) {
+    table.t[i] = t[i];
+    table.t[i].first_group = (uint32_t)groups;
+    groups += cdiv(t[i].n, ADAMW_SPAN);
+  }
+  if (a.eight) adamw_k<true><<<(unsigned)groups, THREADS, 0, st>>>(table);
+  else adamw_k<false><<<(unsigned)groups, THREADS, 0, st>>>(table);
+  return hipGetLastError();
+}
+
+// ---- norm -------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, WAVE);
+  return v;
+}
+template <int N>
+__device__ __forceinline__ double group_sum(double v) {      // of N threads, the same for all of them
+  __shared__ double red[N / WAVE];
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < N / WAVE; ++i) s += red[i];
+  return s;
+}
+
+template <typename G>
+__device__ __forceinline__ double squares(const NormTensor& t, int64_t first, int64_t span) {
+  const G* g = (const G*)t.grad;
+  const bool aligned = ((uintptr_t)g & 15) == 0;
+  const int64_t end = min(first + span, t.n);
+  double sum = 0.0;
+  for (int64_t at = first; at < end; at += TILE) {
+    const int64_t e = at + threadIdx.x * PER;
+    float x[8];
+    if (aligned && at + TILE <= t.n) get<true>(x, g + e, PER);
+    else get<false>(x, g + e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)));
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += x[i] * x[i];
+    sum += (double)s;
+  }
+  return sum;
+}
+__global__ __launch_bounds__(THREADS) void grad_squares_k(const NormTable table) {
+  const NormTensor& t = table.t[tensor_of(table, blockIdx.x)];
+  const int64_t first = (int64_t)(blockIdx.x - t.first_group) * table.span;
+  const double s = group_sum<THREADS>(t.dtype == DT_BF16 ? squares<bf16_t>(t, first, table.span) : squares<float>(t, first, table.span));
+  if (threadIdx.x == 0) table.part[blockIdx.x] = s;
+}
+hipError_t norm_parts(const NormTensor* t, int n, int64_t span, double* part, int* n_parts, hipStream_t st) {
+  if (n < 1 || n > NORM_TABLE || span < TILE || span % TILE) return hipErrorInvalidValue;
+  NormTable table{};
+  table.part = part;
+  table.span = span;
+  table.n = n;
+  int64_t groups = 0;
+  for (int i = 0; i < n; ++i) {
+    table.t[i] = t[i];
+    table.t[i].first_group = (uint32_t)groups;
+    groups += cdiv(t[i].n, span);
+  }
+  grad_squares_k<<<(unsigned)groups, THREADS, 0, st>>>(table);
+  *n_parts = (int)groups;
+  return hipGetLastError();
+}
+
+constexpr int FINISH_THREADS = 1024;
+__global__ __launch_bounds__(FINISH_THREADS) void norm_finish_k(const double* __restrict__ part, int n, float max_norm, float* __restrict__ norm,
+                                                                float* __restrict__ scale) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += FINISH_THREADS) s += part[i];
+  s = group_sum<FINISH_THREADS>(s);
+  if (threadIdx.x != 0) return;
+  const float x = (float)sqrt(s);
+  *norm = x;
+  if (scale) *scale = !(x < INFINITY) ? __builtin_nanf("") : max_norm > 0.f && x > max_norm ? max_norm / x : 1.f;
+}
+hipError_t norm_finish(const double* part, int n, float max_norm, float* norm, float* scale, hipStream_t st) {
+  norm_finish_k<<<1, FINISH_THREADS, 0, st>>>(part, n, max_norm, norm, scale);
+  return hipGetLastError();
+}
+
+}  // namespace sbp
