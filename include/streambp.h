@@ -96,6 +96,9 @@ typedef struct {
   int32_t window;       /* attention mask (Sec. 3.2.2 allows a general mask M, "padding /
                            sliding window"): 0 = plain causal; > 0 = the token at row t
                            attends to rows t - window < u <= t only                 */
+  int32_t sinks;        /* with a window, the first `sinks` tokens of every sequence (from seq_first[b] on) stay visible
+                           to all later ones; without one they are visible anyway.  Zero in
+                           structs of before this field, whose padding bytes are zeroed */
   const int32_t *seq_first; /* HOST array [batch] or NULL: rows of sequence b before
                            seq_first[b] are padding in front of the sequence - never
                            attended to; as queries they attend to nothing, so their
@@ -252,6 +255,10 @@ typedef struct {
   int32_t kv_first;              /* key positions before this one are padding in front of
                                     the sequence: never visible.  A query that sees no key
                                     gets o = 0, lse = -inf and no gradient             */
+  int32_t sinks;                 /* with a window: the key positions kv_first .. kv_first + sinks - 1 stay visible to
+                                    every query at or after them.  bf16, head_dim 128 or 64: of K and V only rows that
+                                    some query of a tile of 256 may see are read, so that what was evicted
+                                    between the sinks and the window may hold anything       */
 } sbp_attn_cfg;
 
 /* What streambp_attn_chunk_backward makes full use of: row statistics, and up to 64 MiB of partial dK/dV where the key

@@ -17,7 +17,9 @@ attn     causal attention of a chunk of queries against the prefix keys and
 lora     the same layer with low-rank adapters on its projection matrices and
          the adapter gradients (App. D, experiment setup: rank-32 adapters for
          the largest model); the masks of attn / layer beyond plain causality
-         (sliding window, padding in front) are options of those modules.
+         (sliding window, padding in front, sinks) are options of those modules.
+optim    AdamW with its 8-bit states and random bits, and the norm of all
+         gradients.
 chunked  the paper's chunk loop itself, in fp64, step by step (Sec. 3.2.1 and
          3.2.2) - used to check that per-chunk partial gradients sum to the
          full gradient and that chunk size does not matter.

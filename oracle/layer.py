@@ -16,8 +16,9 @@ out of the presentation only).  The readings taken here:
     and k before K is cached, scores scaled by 1/sqrt(head_dim), sigma := SiLU.
   * weights are stored [out, in]; y = x W^T.
 
-  * the mask M is causal by default; cfg may add the two further rules of
-    oracle/attn.py: "window" (sliding window, 0 = off) and "first_valid"
+  * the mask M is causal by default; cfg may add the further rules of
+    oracle/attn.py: "window" (sliding window, 0 = off), "sinks" (first positions
+    that stay visible behind it) and "first_valid"
     (positions before it are padding in front of the sequence: never visible
     as keys; as queries they see nothing, so their attention output is zero).
 
@@ -107,7 +108,8 @@ def layer_forward(x, w, cfg):
     hidden = idx[None, :] > idx[:, None]                 # key index > query index
     window, first = cfg.get("window", 0), cfg.get("first_valid", 0)
     if window > 0:
-        hidden |= idx[None, :] <= idx[:, None] - window  # older than the last `window` positions
+        # older than the last `window` positions, and none of the first ones
+        hidden |= (idx[None, :] <= idx[:, None] - window) & (idx[None, :] >= first + cfg.get("sinks", 0))
     if first > 0:
         hidden |= idx[None, :] < first                   # padding in front of the sequence
     empty = hidden.all(axis=1, keepdims=True)            # queries that see no key (the padding rows themselves)

@@ -139,7 +139,7 @@ int32_t check_layer_cfg(const sbp_layer_cfg* c) {
   if (c->head_dim < 2 || (c->head_dim & 1) || c->head_dim > 256)
     return fail(SBP_ERR_SHAPE, "head_dim must be even and in [2, 256]");
   if (!(c->rms_eps >= 0.f) || !(c->rope_theta > 0.f)) return fail(SBP_ERR_SHAPE, "rms_eps must be >= 0 and rope_theta > 0");
-  if (c->window < 0) return fail(SBP_ERR_SHAPE, "window must be >= 0");
+  if (c->window < 0 || c->sinks < 0) return fail(SBP_ERR_SHAPE, "window and sinks must be >= 0");
   if (c->seq_first)
     for (int b = 0; b < c->batch; ++b)
       if (c->seq_first[b] < 0 || c->seq_first[b] > c->seq_len)
@@ -376,6 +376,7 @@ AttnArgs pass_attn(const sbp_layer_cfg* c, const LayerWs& s, const Pass& p) {
   aa.batch = p.seqs; aa.q_start = p.r0; aa.q_len = p.n; aa.scale = 1.0f / std::sqrt((float)c->head_dim);
   aa.window = c->window; aa.kv_first = c->seq_first ? *std::min_element(c->seq_first + p.b0, c->seq_first + p.b0 + p.seqs) : 0;      // rows before it are padding in front of the sequence
   aa.kv_firsts = c->seq_first && p.seqs > 1 ? c->seq_first + p.b0 : nullptr;
+  attn_set_sinks(aa, c->sinks);
   aa.q = s.q; aa.k = s.K; aa.v = s.V; aa.o = s.o; aa.lse = s.lse;
   if (fusion_mask() & FUSE_ROPE_Q) aa.rope_q = s.rope + (size_t)p.r0 * (c->head_dim / 2);
   return aa;
@@ -503,8 +504,11 @@ int32_t layer_backward_impl(const sbp_layer_cfg* c, const sbp_layer_weights* w, 
       HIPCHK(gemm(dx_gemm(s.dh1_t, w->wo, s.d_o, n, d, qd, dt, dt, false), st));
       AttnArgs aa = pass_attn(c, s, p);            // (with rope_q dq leaves the kernel rotated back, RoPE's adjoint)
       aa.d_o = s.d_o; aa.dq = s.dq; aa.dk = s.dK; aa.dv = s.dV; aa.delta = s.delta;
-      if (dt == DT_BF16) aa.dkv_slices = attn_dkv_slices(aa, s.gemm_scratch_bytes);
-      if (aa.dkv_slices > 1) aa.dkv_scratch = s.gemm_scratch;                                   // (idle between GEMMs)
+      if (dt == DT_BF16) {
+        aa.dkv_slices = attn_dkv_slices(aa, s.gemm_scratch_bytes);
+        aa.sink_slices = attn_sink_slices(aa, s.gemm_scratch_bytes);
+      }
+      if (aa.dkv_slices > 1 || aa.sink_slices > 1) aa.dkv_scratch = s.gemm_scratch;                                   // (idle between GEMMs)
       // K/V side of the pass's rows: final now
       aa.dkc = s.dkc; aa.dvc = s.dvc; aa.rope_k = s.rope + (size_t)p.r0 * half;
       HIPCHK(attn_backward(aa, st));
@@ -1019,7 +1023,7 @@ static int32_t check_attn_cfg(const sbp_attn_cfg* c) {
   if ((int64_t)c->q_start + c->q_len > INT32_MAX) return fail(SBP_ERR_SHAPE, "q_start + q_len overflows");
   // the kernels take row maxima of the raw scores before scaling them, which is only right for a positive finite scale
   if (!(c->scale > 0.f) || !std::isfinite(c->scale)) return fail(SBP_ERR_SHAPE, "scale must be positive and finite");
-  if (c->window < 0 || c->kv_first < 0) return fail(SBP_ERR_SHAPE, "window and kv_first must be >= 0");
+  if (c->window < 0 || c->kv_first < 0 || c->sinks < 0) return fail(SBP_ERR_SHAPE, "window, kv_first and sinks must be >= 0");
   return SBP_OK;
 }
 
@@ -1029,14 +1033,18 @@ static AttnArgs attn_args(const sbp_attn_cfg* c) {
   AttnArgs a{};
   a.dt = c->dtype; a.Hq = c->n_q_heads; a.Hkv = c->n_kv_heads; a.dh = c->head_dim;
   a.q_start = c->q_start; a.q_len = c->q_len; a.scale = c->scale; a.window = c->window; a.kv_first = c->kv_first;
-  if (c->dtype == SBP_BF16 && (c->head_dim == 128 || c->head_dim == 64)) a.dkv_slices = attn_dkv_slices(a, SIZE_MAX);
+  attn_set_sinks(a, c->sinks);
+  if (c->dtype == SBP_BF16 && (c->head_dim == 128 || c->head_dim == 64)) {
+    a.dkv_slices = attn_dkv_slices(a, SIZE_MAX);
+    a.sink_slices = attn_sink_slices(a, SIZE_MAX);
+  }
   return a;
 }
 
 size_t streambp_attn_workspace_bytes(const sbp_attn_cfg* cfg) {
   if (check_attn_cfg(cfg) != SBP_OK) return 0;
   const AttnArgs a = attn_args(cfg);
-  return attn_stats_bytes(cfg) + align_up(attn_dkv_scratch_bytes(a, a.dkv_slices), 256);
+  return attn_stats_bytes(cfg) + align_up(std::max(attn_dkv_scratch_bytes(a, a.dkv_slices), attn_sink_scratch_bytes(a, a.sink_slices)), 256);
 }
 
 int32_t streambp_attn_chunk_forward(const sbp_attn_cfg* c, const void* q, const void* k, const void* v, void* o,
@@ -1063,7 +1071,7 @@ int32_t streambp_attn_chunk_backward(const sbp_attn_cfg* c, const void* q, const
   if (workspace_bytes < attn_stats_bytes(c)) return fail(SBP_ERR_WORKSPACE, "workspace too small");
   AttnArgs a = attn_args(c);
   // with less than the query's bytes the same slices run one after the other: the same results
-  if (a.dkv_slices > 1 && workspace_bytes >= streambp_attn_workspace_bytes(c)) a.dkv_scratch = (float*)((char*)workspace + attn_stats_bytes(c));
+  if ((a.dkv_slices > 1 || a.sink_slices > 1) && workspace_bytes >= streambp_attn_workspace_bytes(c)) a.dkv_scratch = (float*)((char*)workspace + attn_stats_bytes(c));
   a.q = q; a.k = k; a.v = v; a.o = (void*)o; a.lse = (float*)lse;
   a.d_o = d_o; a.dq = dq; a.dk = dk; a.dv = dv; a.delta = (float*)workspace;
   HIPCHK(attn_backward(a, (hipStream_t)hip_stream));

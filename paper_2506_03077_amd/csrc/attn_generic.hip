@@ -181,8 +181,23 @@ __device__ __forceinline__ void exchange(f32x4* x, int turn, int slot, int share
   }
 }
 
-struct AgShape { int Hq, Hkv, dh, q_start, c; float scale; int window, kv_first; };
+struct AgShape { int Hq, Hkv, dh, q_start, c; float scale; int window, kv_first, sinks; };
 __device__ __forceinline__ int first_key(const AgShape& a, int pos) { return max(a.kv_first, a.window > 0 ? pos - a.window + 1 : 0); }
+// SINKS: the first `sinks` keys from kv_first on stay visible behind the window.  The blocks that hold them come before those from b0 on, the window's: places b0 - n_sink
+// to b0 - 1 of a walk stand for them.
+template <bool SINKS>
+struct KeyBlocks {
+  int b0, sink0 = 0, n_sink = 0;
+  __device__ __forceinline__ KeyBlocks(const AgShape& a, int first, int end) : b0(first) {
+    if constexpr (SINKS) {
+      sink0 = a.kv_first / 16;
+      n_sink = max(0, min(min((a.kv_first + a.sinks + 15) / 16, b0), end) - sink0);
+    }
+  }
+  __device__ __forceinline__ int start() const { return b0 - n_sink; }
+  __device__ __forceinline__ int at(int b) const { return SINKS && b < b0 ? sink0 + b - start() : b; }
+};
+__device__ __forceinline__ bool is_sink(const AgShape& a, int u) { return u >= a.kv_first && u - a.kv_first < a.sinks; }
 
 // What a wave is: a slot takes every SLOTS-th block, its waves a share of the head each
 #define AG_WAVE_SETUP                                                                                             \
@@ -197,9 +212,9 @@ __device__ __forceinline__ int first_key(const AgShape& a, int pos) { return max
 #define AG_PARTS(N) __shared__ __attribute__((aligned(16))) float part[(N) * Parts<DB, P, W>::FLOATS]
 
 // ---- forward.  rope: q arrives un-rotated, is rotated on load and written back rotated.
-template <typename T, int DB, int P, int W>
-__global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __restrict__ k, const T* __restrict__ v, T* __restrict__ o,
-                                                                 float* __restrict__ lse, AgShape a, const float2* __restrict__ rope) {
+template <typename T, int DB, int P, int W, bool SINKS>
+__device__ __forceinline__ void fwd_block(T* q, const T* __restrict__ k, const T* __restrict__ v, T* __restrict__ o, float* __restrict__ lse, AgShape a,
+                                          const float2* __restrict__ rope) {
   AG_PARTS(1);
   AG_WAVE_SETUP;
   __shared__ f32x4 sX[EXCHANGE<P, 1, W>];
@@ -210,6 +225,7 @@ __global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __re
   const int t = min(t0 + li, a.c - 1), pos = a.q_start + t;                    // my query
   const int lo = first_key(a, pos), n_keys = a.q_start + min(t0 + 16, a.c);
   const int b0 = first_key(a, a.q_start + t0) / 16, b1 = (n_keys + 15) / 16;
+  const KeyBlocks<SINKS> blocks(a, b0, b1);
   const int lo_last = first_key(a, a.q_start + min(t0 + 15, a.c - 1));
   auto q_row = [&](int row) { return q + ((int64_t)min(t0 + row, a.c - 1) * a.Hq + h) * a.dh; };
   typename Raw<T>::four kr[DB];
@@ -219,8 +235,8 @@ __global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __re
   f32x4 qf[DB];
   typename Raw<T>::four raw[DB];
   if (!rope) load_row<T, DB>(raw, q_row(0), min(li, a.c - 1 - t0), a.Hq * a.dh, FIRST, d0, lg4, a.dh);
-  int b = b0 + slot;
-  if (b < b1) { load_k(b * 16); load_v(b * 16); }      // the first block is under way before q is waited for
+  int b = blocks.start() + slot;
+  if (b < b1) { load_k(blocks.at(b) * 16); load_v(blocks.at(b) * 16); }      // the first block is under way before q is waited for
   if (rope) {
     const int half = a.dh / 2;
     constexpr int N = (16 * Pt::HEAD * 16 + Pt::THREADS - 1) / Pt::THREADS;
@@ -256,9 +272,9 @@ __global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __re
   f32x4 acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int rounds = AG_ROUNDS(b1 - b0);
+  const int rounds = AG_ROUNDS(b1 - blocks.start());
   for (int n = 0; n < rounds; ++n, b += SLOTS) {
-    const int u0 = b * 16, next = b + SLOTS;
+    const int u0 = blocks.at(b) * 16, next = b + SLOTS;
     const bool on = P == 1 || b < b1;
     f32x4 sc[1] = {{0.f, 0.f, 0.f, 0.f}};
     f32x4& s = sc[0];
@@ -269,7 +285,7 @@ __global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __re
 #pragma unroll
         for (int j = 0; j < 4; ++j) s = AG_MFMA(kd[j], qf[d][j], s);
       }
-      if (next < b1) load_k(next * 16);
+      if (next < b1) load_k(blocks.at(next) * 16);
     }
     exchange<P, 1, W>(sX, n, slot, share, on, sc);
     if (!on) continue;
@@ -279,7 +295,7 @@ __global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __re
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int u = u0 + lg4 + r;
-      seen[r] = u <= pos && u >= lo;
+      seen[r] = SINKS ? u <= pos && (u >= lo || is_sink(a, u)) : u <= pos && u >= lo;
       s[r] = seen[r] ? s[r] : -INFINITY;
       mx = fmaxf(mx, s[r]);
     }
@@ -298,7 +314,7 @@ __global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __re
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] *= corr;
     second_product<T, DB>(acc, d0, vr, s, edge, seen, a.dh, [&](int row, int e) { return ldf(vb + (int64_t)min(u0 + row, n_keys - 1) * kv_stride + e); });
-    if (next < b1) load_v(next * 16);
+    if (next < b1) load_v(blocks.at(next) * 16);
   }
   // acc[d][r]: element (d0 + d) * 16 + 4 lg + r of O of query li
   l = over_groups(l);
@@ -336,9 +352,19 @@ __global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __re
     if (p.e + half < a.dh) stf(out + half, lt > 0.f ? y[n] / lt : 0.f);
   }
 }
+template <typename T, int DB, int P, int W>
+__global__ __launch_bounds__(W * 64) void attn_fwd_generic_k(T* q, const T* __restrict__ k, const T* __restrict__ v, T* __restrict__ o,
+                                                                 float* __restrict__ lse, AgShape a, const float2* __restrict__ rope) {
+  fwd_block<T, DB, P, W, false>(q, k, v, o, lse, a, rope);
+}
+template <typename T, int DB, int P, int W>
+__global__ __launch_bounds__(W * 64) void attn_fwd_sinks_any_k(T* q, const T* __restrict__ k, const T* __restrict__ v, T* __restrict__ o,
+                                                               float* __restrict__ lse, AgShape a, const float2* __restrict__ rope) {
+  fwd_block<T, DB, P, W, true>(q, k, v, o, lse, a, rope);
+}
 
 // ---- dQ; also delta[h, t] = sum_j d_o[t,h,j] * o[t,h,j], which dK/dV reads.  rope: dq leaves rotated back.
-template <typename T, int DB, int P, int W>
+template <typename T, int DB, int P, int W, bool SINKS = false>
 __device__ __forceinline__ void dq_block(float* part, int tile, int h, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
                                          const T* __restrict__ o, const T* __restrict__ d_o, const float* __restrict__ lse, float* __restrict__ delta,
                                          T* __restrict__ dq, const AgShape& a, const float2* __restrict__ rope) {
@@ -351,6 +377,7 @@ __device__ __forceinline__ void dq_block(float* part, int tile, int h, const T* 
   const int t = min(t0 + li, a.c - 1), pos = a.q_start + t;
   const int lo = first_key(a, pos), n_keys = a.q_start + min(t0 + 16, a.c);
   const int b0 = first_key(a, a.q_start + t0) / 16, b1 = (n_keys + 15) / 16;
+  const KeyBlocks<SINKS> blocks(a, b0, b1);
   const int lo_last = first_key(a, a.q_start + min(t0 + 15, a.c - 1));
   const int64_t q0 = ((int64_t)t0 * a.Hq + h) * a.dh;
   const int row = min(li, a.c - 1 - t0), q_stride = a.Hq * a.dh;
@@ -368,8 +395,8 @@ __device__ __forceinline__ void dq_block(float* part, int tile, int h, const T* 
     load_row<T, DB>(vr, vb + at, key, kv_stride, FIRST, d0, lg4, a.dh);
   };
   auto load_cols = [&](int u0) { load_across<T, DB>(kt, kb + (int64_t)u0 * kv_stride, lg4, n_keys - 1 - u0, kv_stride, FIRST, d0, li, a.dh); };
-  int b = b0 + slot;
-  if (b < b1) { load_rows(b * 16); load_cols(b * 16); }      // the first block is under way before q is waited for
+  int b = blocks.start() + slot;
+  if (b < b1) { load_rows(blocks.at(b) * 16); load_cols(blocks.at(b) * 16); }      // the first block is under way before q is waited for
   float D = 0.f;
 #pragma unroll
   for (int d = 0; d < DB; ++d) {
@@ -391,9 +418,9 @@ __device__ __forceinline__ void dq_block(float* part, int tile, int h, const T* 
   f32x4 acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int rounds = AG_ROUNDS(b1 - b0);
+  const int rounds = AG_ROUNDS(b1 - blocks.start());
   for (int n = 0; n < rounds; ++n, b += SLOTS) {
-    const int u0 = b * 16, next = b + SLOTS;
+    const int u0 = blocks.at(b) * 16, next = b + SLOTS;
     const bool on = P == 1 || b < b1;
     f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     f32x4 &s = sc[0], &dp = sc[1];
@@ -407,7 +434,7 @@ __device__ __forceinline__ void dq_block(float* part, int tile, int h, const T* 
           dp = AG_MFMA(vd[j], df[d][j], dp);
         }
       }
-      if (next < b1) load_rows(next * 16);
+      if (next < b1) load_rows(blocks.at(next) * 16);
     }
     exchange<P, 2, W>(sX, n, slot, share, on, sc);
     if (!on) continue;
@@ -416,11 +443,11 @@ __device__ __forceinline__ void dq_block(float* part, int tile, int h, const T* 
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int u = u0 + lg4 + r;
-      seen[r] = u <= pos && u >= lo;
+      seen[r] = SINKS ? u <= pos && (u >= lo || is_sink(a, u)) : u <= pos && u >= lo;
       s[r] = seen[r] ? expf(s[r] * a.scale - L) * (dp[r] - D) * a.scale : 0.f;
     }
     second_product<T, DB>(acc, d0, kt, s, edge, seen, a.dh, [&](int row, int e) { return ldf(kb + (int64_t)min(u0 + row, n_keys - 1) * kv_stride + e); });
-    if (next < b1) load_cols(next * 16);
+    if (next < b1) load_cols(blocks.at(next) * 16);
   }
   const int half = (a.dh + 1) / 2;
   Pt::leave(part, slot, d0, acc, li, lg4);
@@ -450,10 +477,19 @@ __global__ __launch_bounds__(W * 64) void attn_dq_generic_k(const T* __restrict_
   AG_PARTS(1);
   dq_block<T, DB, P, W>(part, blockIdx.x, blockIdx.y, q, k, v, o, d_o, lse, delta, dq, a, rope);
 }
+template <typename T, int DB, int P, int W>
+__global__ __launch_bounds__(W * 64) void attn_dq_sinks_any_k(const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+                                                                const T* __restrict__ o, const T* __restrict__ d_o, const float* __restrict__ lse,
+                                                                float* __restrict__ delta, T* __restrict__ dq, AgShape a,
+                                                                const float2* __restrict__ rope) {
+  AG_PARTS(1);
+  dq_block<T, DB, P, W, true>(part, blockIdx.x, blockIdx.y, q, k, v, o, d_o, lse, delta, dq, a, rope);
+}
 
 // ---- dK/dV (and dkc, dvc of the chunk's own rows, final with this call): 16 keys of one KV head; the slots walk blocks of 16 queries that see some of them, for every query head of the group
 // DELTA: D of the queries from d_o and o, as dQ forms it, in place of reading what dQ has left.
-template <typename T, int DB, int P, int W, bool DELTA>
+// SINKS: the queries behind a sink's window are among them, and a block that holds a sink walks all of them.
+template <typename T, int DB, int P, int W, bool DELTA, bool SINKS = false>
 __device__ __forceinline__ void dkv_block(float* part, int block, int kvh, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
                                           const T* __restrict__ o, const T* __restrict__ d_o, const float* __restrict__ lse, const float* __restrict__ delta,
                                           float* __restrict__ dk, float* __restrict__ dv, const AgShape& a, T* __restrict__ dkc, T* __restrict__ dvc,
@@ -466,7 +502,7 @@ __device__ __forceinline__ void dkv_block(float* part, int block, int kvh, const
   const int kv_stride = a.Hkv * a.dh, q_stride = a.Hq * a.dh;
   const int t_first = max(0, u0 - a.q_start);                                  // rows before it see none of the keys, nor do rows from t_end on
   int t_end = a.c;
-  if (a.window > 0) t_end = (int)min((int64_t)a.c, max((int64_t)0, (int64_t)u0 + 15 + a.window - a.q_start));
+  if (a.window > 0 && !(SINKS && u0 + 15 >= a.kv_first && u0 - a.kv_first < a.sinks)) t_end = (int)min((int64_t)a.c, max((int64_t)0, (int64_t)u0 + 15 + a.window - a.q_start));
   if (u0 + 15 < a.kv_first) t_end = 0;
   const int b0 = t_first / 16, n_it = max(0, (t_end + 15) / 16 - b0) * G;
   typename Raw<T>::four qr[DB], dr[DB], orow[DELTA ? DB : 1], raw_k[DB], raw_v[DB];
@@ -553,7 +589,8 @@ __device__ __forceinline__ void dkv_block(float* part, int block, int kvh, const
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int t = t0 + lg4 + r, pos = a.q_start + t;
-      seen[r] = t < a.c && u0 + li < n_total && u <= pos && u >= first_key(a, pos);
+      if constexpr (SINKS) seen[r] = t < a.c && u0 + li < n_total && u <= pos && (u >= first_key(a, pos) || is_sink(a, u));
+      else seen[r] = t < a.c && u0 + li < n_total && u <= pos && u >= first_key(a, pos);
       const float p = seen[r] ? expf(s[r] * a.scale - L[r]) : 0.f;
       s[r] = p;
       dp[r] = seen[r] ? p * (dp[r] - D[r]) * a.scale : 0.f;
@@ -610,6 +647,14 @@ __global__ __launch_bounds__(W * 64, DB * P == 8 ? 4 : 1) void attn_dkv_generic_
   AG_PARTS(2);
   dkv_block<T, DB, P, W, false>(part, blockIdx.x, blockIdx.y, q, k, v, nullptr, d_o, lse, delta, dk, dv, a, dkc, dvc, rope);
 }
+template <typename T, int DB, int P, int W>
+__global__ __launch_bounds__(W * 64, DB * P == 8 ? 4 : 1) void attn_dkv_sinks_any_k(const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+                                                                                  const T* __restrict__ d_o, const float* __restrict__ lse,
+                                                                                  const float* __restrict__ delta, float* __restrict__ dk, float* __restrict__ dv,
+                                                                                  AgShape a, T* __restrict__ dkc, T* __restrict__ dvc, const float2* __restrict__ rope) {
+  AG_PARTS(2);
+  dkv_block<T, DB, P, W, false, true>(part, blockIdx.x, blockIdx.y, q, k, v, nullptr, d_o, lse, delta, dk, dv, a, dkc, dvc, rope);
+}
 // dK/dV and dQ side by side, neither waiting for the other: the workgroups of dK/dV form delta themselves, the same sums in the same order.
 template <typename T, int DB>
 __global__ __launch_bounds__(512) void attn_bwd_narrow_k(const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, const T* __restrict__ o,
@@ -623,8 +668,20 @@ __global__ __launch_bounds__(512) void attn_bwd_narrow_k(const T* __restrict__ q
   if (first != dq_first) dkv_block<T, DB, P, W, true>(part, b / a.Hkv, b % a.Hkv, q, k, v, o, d_o, lse, nullptr, dk, dv, a, dkc, dvc, rope_k);
   else dq_block<T, DB, P, W>(part, b / a.Hq, b % a.Hq, q, k, v, o, d_o, lse, nullptr, dq, a, rope_q);
 }
+template <typename T, int DB>
+__global__ __launch_bounds__(512) void attn_bwd_narrow_sinks_k(const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, const T* __restrict__ o,
+                                                          const T* __restrict__ d_o, const float* __restrict__ lse, T* __restrict__ dq, float* __restrict__ dk,
+                                                          float* __restrict__ dv, AgShape a, T* __restrict__ dkc, T* __restrict__ dvc,
+                                                          const float2* __restrict__ rope_q, const float2* __restrict__ rope_k, int n_first, bool dq_first) {
+  constexpr int P = 1, W = 8;
+  AG_PARTS(2);
+  const bool first = (int)blockIdx.x < n_first;
+  const int b = (int)blockIdx.x - (first ? 0 : n_first);
+  if (first != dq_first) dkv_block<T, DB, P, W, true, true>(part, b / a.Hkv, b % a.Hkv, q, k, v, o, d_o, lse, nullptr, dk, dv, a, dkc, dvc, rope_k);
+  else dq_block<T, DB, P, W, true>(part, b / a.Hq, b % a.Hq, q, k, v, o, d_o, lse, nullptr, dq, a, rope_q);
+}
 
-static AgShape shape_of(const AttnArgs& a) { return AgShape{a.Hq, a.Hkv, a.dh, a.q_start, a.q_len, a.scale, a.window, a.kv_first}; }
+static AgShape shape_of(const AttnArgs& a) { return AgShape{a.Hq, a.Hkv, a.dh, a.q_start, a.q_len, a.scale, a.window, a.kv_first, a.sinks}; }
 // Instances: pieces per wave, waves per block, waves.  Heads of up to 64 elements: one wave per block.  Wider ones, whose operands would not fit a wave's
 // registers: two, or four - where there are few blocks, where the registers of two would spill (dK/dV, dQ of more than 160 elements), and, on sixteen waves, in
 // the forward of more than 160.  Forward, 4 heads, 64 / 256 / 512 / 2112 keys, 64 queries, fp32, two per block and four, in us: heads of 80 7 11 17 58 and 8 15 27
@@ -663,7 +720,9 @@ static hipError_t forward_t(const AttnArgs& a, hipStream_t st) {
   const AgShape s = shape_of(a);
   const dim3 grid((unsigned)cdiv(a.q_len, 16), (unsigned)a.Hq);
   auto go = [&](auto db, auto p, auto w) {
-    attn_fwd_generic_k<T, decltype(db)::value, decltype(p)::value, decltype(w)::value><<<grid, decltype(w)::value * 64, 0, st>>>((T*)a.q, (const T*)a.k, (const T*)a.v, (T*)a.o, a.lse, s, a.rope_q);
+    constexpr int DB = decltype(db)::value, P = decltype(p)::value, W = decltype(w)::value;
+    auto launch = [&](auto kernel) { kernel<<<grid, W * 64, 0, st>>>((T*)a.q, (const T*)a.k, (const T*)a.v, (T*)a.o, a.lse, s, a.rope_q); };
+    if (a.sinks > 0) launch(attn_fwd_sinks_any_k<T, DB, P, W>); else launch(attn_fwd_generic_k<T, DB, P, W>);
   };
   if (a.dh <= 64) narrow_heads(a.dh, go); else if (few_keys(a)) four_per_block(a.dh, go); else forward_long(a.dh, go);
   return hipGetLastError();
@@ -675,19 +734,27 @@ static hipError_t backward_t(const AttnArgs& a, hipStream_t st) {
   const AttnNarrowPlan p = attn_narrow_plan(a);
   if (p.one_launch) {
     narrow_heads(a.dh, [&](auto db, auto, auto) {
-      attn_bwd_narrow_k<T, decltype(db)::value><<<(unsigned)(p.n_dkv + p.n_dq), 512, 0, st>>>((const T*)a.q, (const T*)a.k, (const T*)a.v, (const T*)a.o, (const T*)a.d_o, a.lse, (T*)a.dq,
-                                                                            a.dk, a.dv, s, (T*)a.dkc, (T*)a.dvc, a.rope_q, a.rope_k, (int)(p.dq_first ? p.n_dq : p.n_dkv), p.dq_first);
+      constexpr int DB = decltype(db)::value;
+      auto launch = [&](auto kernel) {
+        kernel<<<(unsigned)(p.n_dkv + p.n_dq), 512, 0, st>>>((const T*)a.q, (const T*)a.k, (const T*)a.v, (const T*)a.o, (const T*)a.d_o, a.lse, (T*)a.dq, a.dk, a.dv, s,
+                                                             (T*)a.dkc, (T*)a.dvc, a.rope_q, a.rope_k, (int)(p.dq_first ? p.n_dq : p.n_dkv), p.dq_first);
+      };
+      if (a.sinks > 0) launch(attn_bwd_narrow_sinks_k<T, DB>); else launch(attn_bwd_narrow_k<T, DB>);
     });
     return hipGetLastError();
   }
   auto dq = [&](auto db, auto p, auto w) {
-    attn_dq_generic_k<T, decltype(db)::value, decltype(p)::value, decltype(w)::value><<<gq, decltype(w)::value * 64, 0, st>>>((const T*)a.q, (const T*)a.k, (const T*)a.v, (const T*)a.o, (const T*)a.d_o,
-                                                                                        a.lse, a.delta, (T*)a.dq, s, a.rope_q);
+    constexpr int DB = decltype(db)::value, P = decltype(p)::value, W = decltype(w)::value;
+    auto launch = [&](auto kernel) { kernel<<<gq, W * 64, 0, st>>>((const T*)a.q, (const T*)a.k, (const T*)a.v, (const T*)a.o, (const T*)a.d_o, a.lse, a.delta, (T*)a.dq, s, a.rope_q); };
+    if (a.sinks > 0) launch(attn_dq_sinks_any_k<T, DB, P, W>); else launch(attn_dq_generic_k<T, DB, P, W>);
   };
   if (a.dh <= 64) narrow_heads(a.dh, dq); else if (few_keys(a)) four_per_block(a.dh, dq); else dq_long(a.dh, dq);
   auto dkv = [&](auto db, auto p, auto w) {
-    attn_dkv_generic_k<T, decltype(db)::value, decltype(p)::value, decltype(w)::value><<<gk, decltype(w)::value * 64, 0, st>>>((const T*)a.q, (const T*)a.k, (const T*)a.v, (const T*)a.d_o, a.lse, a.delta,
-                                                                                         a.dk, a.dv, s, (T*)a.dkc, (T*)a.dvc, a.rope_k);
+    constexpr int DB = decltype(db)::value, P = decltype(p)::value, W = decltype(w)::value;
+    auto launch = [&](auto kernel) {
+      kernel<<<gk, W * 64, 0, st>>>((const T*)a.q, (const T*)a.k, (const T*)a.v, (const T*)a.d_o, a.lse, a.delta, a.dk, a.dv, s, (T*)a.dkc, (T*)a.dvc, a.rope_k);
+    };
+    if (a.sinks > 0) launch(attn_dkv_sinks_any_k<T, DB, P, W>); else launch(attn_dkv_generic_k<T, DB, P, W>);
   };
   if (a.dh <= 64) narrow_heads(a.dh, dkv); else four_per_block(a.dh, dkv);
   return hipGetLastError();

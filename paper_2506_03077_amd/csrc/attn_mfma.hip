@@ -229,6 +229,46 @@ __device__ __forceinline__ void query_tile_of(int id, int n_qt, int heads, int& 
   qt = n_qt - 1 - row;
 }
 
+// The key tiles of a workgroup's queries: those from kt0 on, the first that any of them sees in its window, up to n_tiles.  SINKS: before them those
+// of the first `sinks` keys from kv_first on, which every later query sees, as far as they lie before kt0.  A sink is one key more for the softmax and
+// for every product, so nothing else of the walk changes: tiles that a wave sees nothing of, which its workgroup walks between the sinks and the wave's own
+// window, are masked as a whole (a barrier paces the waves, so that skipping them would gain nothing).  The sinks may end in a tile from kt0 on, so every wave begins
+// with the first one.
+template <bool SINKS, int NK>
+struct KeyTiles {
+  int kt0, n_window, sink0 = 0, n_sink = 0, kv_first, sink_end;      // keys kv_first .. sink_end - 1 are the sinks
+  __device__ __forceinline__ KeyTiles(int first, int sinks, int first_tile, int n_tiles, int n_total)
+      : kt0(first_tile), n_window(max(0, n_tiles - first_tile)), kv_first(first), sink_end(first + min(sinks, max(0, n_total - first))) {
+    if constexpr (SINKS) {
+      sink0 = first / NK;
+      n_sink = max(0, min(min((sink_end + NK - 1) / NK, kt0), n_tiles) - sink0);
+    }
+  }
+  __device__ __forceinline__ int n() const { return n_sink + n_window; }
+  __device__ __forceinline__ int at(int i) const { return SINKS && i < n_sink ? sink0 + i : kt0 - n_sink + i; }
+  __device__ __forceinline__ int base() const { return kt0 - n_sink; }      // of the window's tiles: at(i) - i
+  // A row of tile t that some query may see in the place of one that none of the workgroup does (before the first key, between the sinks and `lo`, the first key of
+  // the windows, behind the last key): what lies there is never read.
+  __device__ __forceinline__ int safe_row(int t, int row, int lo, int rows_valid) const {
+    const int gap = sink_end - t * NK, end = lo - t * NK;
+    if (row >= gap && row < end) row = end < NK ? end : max(gap, 1) - 1;
+    return min(max(row, kv_first - t * NK), rows_valid - 1);
+  }
+};
+// Key 4 lg + e of a tile is visible to a query for first <= e < first + n (its window), or, SINKS, sink <= e < sink + n_sink: one unsigned comparison each
+template <bool SINKS>
+struct Seen {
+  int first, sink = 0;
+  uint32_t n, n_sink = 0;
+  __device__ __forceinline__ Seen(int qpos, int lo, int kv_first, int sink_end, int key0) : first(lo - key0), n((uint32_t)max(0, qpos - lo + 1)) {
+    if constexpr (SINKS) {
+      sink = kv_first - key0;
+      n_sink = (uint32_t)max(0, min(sink_end, qpos + 1) - kv_first);
+    }
+  }
+  __device__ __forceinline__ bool operator()(int e) const { return (uint32_t)(e - first) < n || (SINKS && (uint32_t)(e - sink) < n_sink); }
+};
+
 // ------------------------------------------------------------------ forward --
 // 8 waves in two groups of four; waves w and w + 4 share a SIMD.  A key tile costs a wave two slots, each closed by a barrier:
 // multiply (O += P V of the previous tile, S = K Q^T of this one: 68 MFMAs, the softmax denominator - at DH = 128 one product against
@@ -249,12 +289,12 @@ __device__ __forceinline__ void query_tile_of(int id, int n_qt, int heads, int& 
 // that chunk, 777 windowed queries 31.9 -> 31.1.  Half of its LDS reads left out 739, its exponentials 789, a quarter of the products 710.
 // Tried with a maximum that lags by up to 2^8, itself 921 us but another rounding of every probability: 32x32x16 MFMAs in the same
 // schedule 965, loads in the multiply slot 954, the next slot's first fragments read early 958.
-template <int DH, bool SPLIT>
-__global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const bf16_t* __restrict__ k,
-                                                                 const bf16_t* __restrict__ v, bf16_t* __restrict__ o,
-                                                                 float* __restrict__ lse, int Hq, int Hkv, int q_start,
-                                                                 int c, float scale, const float2* __restrict__ rope,
-                                                                 int window, const AttnSeqs seqs) {
+// SINKS: see KeyTiles.  The denominator sums the fp32 probabilities for heads of 128 too, so that the log-sum-exp is that of fp32.
+template <int DH, bool SPLIT, bool SINKS>
+__device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, bf16_t* __restrict__ o,
+                                         float* __restrict__ lse, int Hq, int Hkv, int q_start, int c, float scale, const float2* __restrict__ rope,
+                                         int window, const AttnSeqs& seqs, int sinks) {
+  constexpr bool SUM32 = FP32_STATS<DH> || SINKS;
   __shared__ __attribute__((aligned(1024))) char sT[8 * TILE64<DH>];   // K stages, then V stages
   __shared__ float sM[SPLIT ? 2 : 1][4][32];                  // SPLIT: the running maxima of the groups' queries
   constexpr int QW = SPLIT ? TQ / 2 : TQ;                     // queries of the workgroup
@@ -282,9 +322,10 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
   auto first_key = [&](int p) { return max(kv_first, window > 0 ? p - window + 1 : 0); };
   const int wave_lo_min = first_key(wave_first_qpos);                 // lowest first key in the wave (its first query)
   const int wave_lo_max = first_key(wave_last_key);                   // highest one (its last query)
-  const int kt0 = first_key(q_start + q0) / TK;                       // first key tile any query of the workgroup sees
-  const int n_it = SPLIT ? (max(0, n_tiles - kt0) + 1) / 2 : max(0, n_tiles - kt0);
-  auto tile_of = [&](int i) { return SPLIT ? kt0 + 2 * i + grp : kt0 + i; };
+  const int kt0 = first_key(q_start + q0) / TK;                       // first key tile any query of the workgroup sees (SINKS: in its window)
+  const KeyTiles<SINKS, TK> tiles(kv_first, sinks, kt0, n_tiles, n_total);
+  const int n_it = SPLIT ? (tiles.n() + 1) / 2 : tiles.n();
+  auto tile_of = [&](int i) { return tiles.at(SPLIT ? 2 * i + grp : i); };
 
   constexpr int KS = DH / 32, DB = DH / 16;                   // k32 steps of a score, 16-row blocks of the output
   bf16x8 bq[2][KS];      // [16-query block][k32 step]: B operands of S^T = K Q^T
@@ -310,8 +351,8 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
         for (int e = 0; e < 8; ++e) {
           const float2 cs = tr[kk * 32 + e];
           const float x1 = (float)bq[b][kk][e], x2 = (float)bq[b][kk + KS / 2][e];
-          bq[b][kk][e] = (bf16_t)(x1 * cs.x - x2 * cs.y);
-          bq[b][kk + KS / 2][e] = (bf16_t)(x2 * cs.x + x1 * cs.y);
+          bq[b][kk][e] = (bf16_t)__builtin_fmaf(x1, cs.x, -(x2 * cs.y));      // (which product is rounded is not left to the compiler: every instance gives the same bits)
+          bq[b][kk + KS / 2][e] = (bf16_t)__builtin_fmaf(x1, cs.y, x2 * cs.x);
         }
       if (my_q < c && (!SPLIT || grp == 0)) {
         bf16_t* qp = q + ((int64_t)my_q * Hq + h) * DH + lg * 8;
@@ -347,8 +388,15 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
     const bool is_k = p >= LOADS;
     const int j = p % LOADS, ahead = is_k ? K_AHEAD : V_AHEAD, t = min(tile_of(i + ahead), t_max);
     const char* src = (const char*)(is_k ? kbase : vbase) + (uint64_t)tile_bytes * (uint32_t)t;
-    dma16(src, t == t_max ? voff_last[j] : voff[j],
-          dst_k + (uint32_t)(((is_k ? 0 : 4) + (i + ahead) % STAGES) * TILE64<DH> + j * LOADERS * 16));
+    const uint32_t to = dst_k + (uint32_t)(((is_k ? 0 : 4) + (i + ahead) % STAGES) * TILE64<DH> + j * LOADERS * 16);
+    if constexpr (SINKS) {
+      if (t <= kt0) {
+        const int id = j * LOADERS + ((int)pin(threadIdx.x) & (LOADERS - 1)), row = id / (DH / 8), chunk = (id % (DH / 8)) ^ swz<DH>(row);      // (opaque: nothing of this is kept in a register)
+        dma16(src, (uint32_t)((tiles.safe_row(t, row, first_key(q_start + q0), n_total - t * TK) * kv_stride + chunk * 8) * 2), to);
+        return;
+      }
+    }
+    dma16(src, t == t_max ? voff_last[j] : voff[j], to);
   };
 
   bf16x8 ones;
@@ -372,8 +420,8 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
   }
   const float sl = scale * LOG2E;
   // steps in which some (query, key) pair of the wave is visible: tiles wave_lo_min / TK .. wave_last_key / TK
-  const int step_t = SPLIT ? 2 : 1, first_t = tile_of(0);
-  const int act0 = max(0, (wave_lo_min / TK - first_t + step_t - 1) / step_t);
+  const int step_t = SPLIT ? 2 : 1, first_t = tiles.base() + (SPLIT ? grp : 0);
+  const int act0 = SINKS ? 0 : max(0, (wave_lo_min / TK - first_t + step_t - 1) / step_t);
   const int act1 = qw0 < c && wave_last_key >= 0 ? min(n_it, (wave_last_key / TK - first_t + step_t) / step_t) : 0;
 
   // LDS addresses of fragments, one step after the other: of K rows of the present tile, of V transposed of the previous one
@@ -404,7 +452,7 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
 #pragma unroll
         for (int t = 0; t < TERMS<DH>; ++t) {
           acc[b][n % DB] = MFMA16(f[n % RING], pb[t][b][n / DB], acc[b][n % DB]);
-          if (!FP32_STATS<DH> && n % DB == DB - 1) acc_l[b] = MFMA16(ones, pb[t][b][n / DB], acc_l[b]);
+          if (!SUM32 && n % DB == DB - 1) acc_l[b] = MFMA16(ones, pb[t][b][n / DB], acc_l[b]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -437,14 +485,12 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
     if (k0 + TK - 1 > wave_first_qpos || k0 < wave_lo_max) {   // only tiles on an edge of the visible range pay for the mask
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        // key 4 lg + e of the tile is visible for first <= e < first + n: one unsigned comparison
-        const int qpos = q_start + min(qw0 + b * 16 + li, c - 1), lo = first_key(qpos);
-        const int first = lo - k0 - 4 * lg;
-        const uint32_t n = (uint32_t)max(0, qpos - lo + 1);
+        const int qpos = q_start + min(qw0 + b * 16 + li, c - 1);
+        const Seen<SINKS> seen(qpos, first_key(qpos), kv_first, tiles.sink_end, k0 + 4 * lg);
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) s[b][kb][r] = (uint32_t)(kb * 16 + r - first) < n ? s[b][kb][r] : -INFINITY;
+          for (int r = 0; r < 4; ++r) s[b][kb][r] = seen(kb * 16 + r) ? s[b][kb][r] : -INFINITY;
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -504,7 +550,7 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
         pb[0][b][kk][e] = (bf16_t)pe[e];
         if (TERMS<DH> == 2) pb[TERMS<DH> - 1][b][kk][e] = (bf16_t)(pe[e] - (float)pb[0][b][kk][e]);
       }
-      if (FP32_STATS<DH>) acc_l[b][0] += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+      if (SUM32) acc_l[b][0] += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -558,7 +604,7 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
     if (grp == 0) AT_SLOT_BARRIER();        // ... and group 0 waits for it here: both execute the same number of barriers
   }
 
-  if constexpr (FP32_STATS<DH>) {      // the four lanes that share a query hold a quarter of its keys each
+  if constexpr (SUM32) {      // the four lanes that share a query hold a quarter of its keys each
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       acc_l[b][0] += __shfl_xor(acc_l[b][0], 16, 64);
@@ -621,6 +667,13 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
     if (lg == 0) lse[(int64_t)h * c + my_q] = !(l_tot > 0.f) ? -INFINITY : FP32_STATS<DH> ? logf(l_tot) - m_neg[b] : (m_raw[b] * sl + log2f(l_tot)) * LN2;
   }
 }
+#define FWD_PARAMS bf16_t *q, const bf16_t *__restrict__ k, const bf16_t *__restrict__ v, bf16_t *__restrict__ o, float *__restrict__ lse, int Hq, int Hkv, \
+                   int q_start, int c, float scale, const float2 *__restrict__ rope, int window, const AttnSeqs seqs
+#define FWD_ARGS q, k, v, o, lse, Hq, Hkv, q_start, c, scale, rope, window, seqs
+template <int DH, bool SPLIT> __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(FWD_PARAMS) { fwd_tile<DH, SPLIT, false>(FWD_ARGS, 0); }
+template <int DH, bool SPLIT> __global__ __launch_bounds__(AT_THREADS) void attn_fwd_sinks_k(FWD_PARAMS, int sinks) { fwd_tile<DH, SPLIT, true>(FWD_ARGS, sinks); }
+#undef FWD_PARAMS
+#undef FWD_ARGS
 
 // ----------------------------------------------------------------------- dQ --
 // The slots of the forward kernel: multiply (dQ^T += K^T dS of the previous tile, S = K Q^T and dP = V dO^T of this one) and vector work (dS, and
@@ -642,11 +695,11 @@ __global__ __launch_bounds__(AT_THREADS) void attn_fwd_mfma_k(bf16_t* q, const b
 template <int DH, bool SPLIT>
 struct DqShared { char sT[8][TILE64<DH>]; };      // K and V of stage after stage; SPLIT: of group 0, then of group 1
 constexpr int DQ_CHAIN = 5;                       // LDS fragments requested ahead of the products (4: the same within 0.3 %)
-template <int DH, bool SPLIT>
+template <int DH, bool SPLIT, bool SINKS = false>
 __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, int bh, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
                                         const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o, const float* __restrict__ lse,
                                         const float* __restrict__ delta, bf16_t* __restrict__ dq, int Hq, int Hkv, int q_start, int c,
-                                        float scale, const float2* __restrict__ rope, int window, const AttnSeqs& seqs) {
+                                        float scale, const float2* __restrict__ rope, int window, const AttnSeqs& seqs, int sinks = 0) {
   auto& sT = sh.sT;
   const int b = bh / Hq, h = bh - b * Hq, kv_first = seqs.first[b];
   q += (int64_t)b * c * Hq * DH; d_o += (int64_t)b * c * Hq * DH; dq += (int64_t)b * c * Hq * DH;
@@ -672,9 +725,10 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
   auto first_key = [&](int p) { return max(kv_first, window > 0 ? p - window + 1 : 0); };   // left edge of the visible range
   const int wave_lo_min = first_key(wave_first_qpos), wave_lo_max = first_key(wave_last_key);
   const int kt0 = first_key(q_start + q0) / NK;
+  const KeyTiles<SINKS, NK> tiles(kv_first, sinks, kt0, n_tiles, n_total);
   // tile i of this wave's sequence
-  auto tile_of = [&](int i) { return SPLIT ? kt0 + 2 * i + grp : kt0 + i; };
-  const int n_it = SPLIT ? (max(0, n_tiles - kt0) + 1) / 2 : max(0, n_tiles - kt0);
+  auto tile_of = [&](int i) { return tiles.at(SPLIT ? 2 * i + grp : i); };
+  const int n_it = SPLIT ? (tiles.n() + 1) / 2 : tiles.n();
 
   constexpr int KS = DH / 32, DB = DH / 16;      // k32 steps of a score, 16-row blocks of the output
   bf16x8 bq[2][KS], bdo[2][KS];                  // [16-query block][k32 step]
@@ -720,6 +774,18 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
     const int t = min(tile_of(i), t_max);
     const char *ks = (const char*)kbase + (uint64_t)tile_bytes * (uint32_t)t, *vs = (const char*)vbase + (uint64_t)tile_bytes * (uint32_t)t;
     const uint32_t to = dst + (uint32_t)(i % STAGES) * STAGE;
+    if constexpr (SINKS) {
+      if (t <= kt0) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const uint32_t id = pin(threadIdx.x) % LOADERS;      // (opaque, as below)
+          const uint32_t off = load_offset(id, (uint32_t)tiles.safe_row(t, (int)(id / (DH / 8)) + j * ROWS_J, first_key(q_start + q0), n_total - t * NK));
+          dma16(ks, off, to + (uint32_t)(j * LOADERS * 16));
+          dma16(vs, off, to + (uint32_t)(TILE + j * LOADERS * 16));
+        }
+        return;
+      }
+    }
     if constexpr (SPLIT) {
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) {
@@ -745,8 +811,8 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
     }
   };
   // steps in which some (query, key) pair of the wave is visible
-  const int step_t = SPLIT ? 2 : 1, first_t = tile_of(0);
-  const int act0 = max(0, (wave_lo_min / NK - first_t + step_t - 1) / step_t);
+  const int step_t = SPLIT ? 2 : 1, first_t = tiles.base() + (SPLIT ? grp : 0);
+  const int act0 = SINKS ? 0 : max(0, (wave_lo_min / NK - first_t + step_t - 1) / step_t);
   const int act1 = qw0 < c && wave_last_key >= 0 ? min(n_it, (wave_last_key / NK - first_t + step_t) / step_t) : 0;
 
   // LDS addresses of fragments, one step after the other: of K (and V) rows of the present tile, of K transposed of the previous one
@@ -809,13 +875,12 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
       const int l = (int)pin(threadIdx.x) & 63;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        // key 4 lg + e of the tile is visible for first <= e < first + n: one unsigned comparison
-        const int qpos = q_start + min(qw0 + b * 16 + (l & 15), c - 1), lo = first_key(qpos), from = lo - k0 - 4 * (l >> 4);
-        const uint32_t n = (uint32_t)max(0, qpos - lo + 1);
+        const int qpos = q_start + min(qw0 + b * 16 + (l & 15), c - 1);
+        const Seen<SINKS> seen(qpos, first_key(qpos), kv_first, tiles.sink_end, k0 + 4 * (l >> 4));
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x.s[b][kb][r] = (uint32_t)(kb * 16 + r - from) < n ? x.s[b][kb][r] : -INFINITY;     // exp2(-inf) = 0
+          for (int r = 0; r < 4; ++r) x.s[b][kb][r] = seen(kb * 16 + r) ? x.s[b][kb][r] : -INFINITY;     // exp2(-inf) = 0
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -957,6 +1022,18 @@ __global__ __launch_bounds__(AT_THREADS) void attn_bwd_dq_mfma_k(const bf16_t* _
   if ((int)gridDim.x > 256) query_tile_of(blockIdx.x, q_blocks, Hq * seqs.n, qt, bh);
   dq_tile<DH, SPLIT>(sh, qt, bh, q, k, v, d_o, lse, delta, dq, Hq, Hkv, q_start, c, scale, rope, window, seqs);
 }
+template <int DH, bool SPLIT>
+__global__ __launch_bounds__(AT_THREADS) void attn_bwd_dq_sinks_k(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
+                                                                  const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o,
+                                                                  const float* __restrict__ lse, const float* __restrict__ delta,
+                                                                  bf16_t* __restrict__ dq, int Hq, int Hkv, int q_start, int c,
+                                                                  float scale, const float2* __restrict__ rope, int window,
+                                                                  const AttnSeqs seqs, int q_blocks, int sinks) {
+  __shared__ __attribute__((aligned(1024))) DqShared<DH, SPLIT> sh;
+  int qt = blockIdx.x % q_blocks, bh = blockIdx.x / q_blocks;
+  if ((int)gridDim.x > 256) query_tile_of(blockIdx.x, q_blocks, Hq * seqs.n, qt, bh);
+  dq_tile<DH, SPLIT, true>(sh, qt, bh, q, k, v, d_o, lse, delta, dq, Hq, Hkv, q_start, c, scale, rope, window, seqs, sinks);
+}
 
 // -------------------------------------------------------------------- dK/dV --
 // Workgroup = 128 keys of one KV head, 8 waves = 4 key blocks of 32 x 2 roles, so that each SIMD holds the two
@@ -983,6 +1060,11 @@ __global__ __launch_bounds__(AT_THREADS) void attn_bwd_dq_mfma_k(const bf16_t* _
 // workgroups share a key block, each with all scores and half of the second product.  Whole backward, without / with a break | one share, dQ
 // apart | with room, 28 / 4 heads: 512 queries from 0 228 / 123 | 143 | 41 us, 2048 from 0 401 / 357 | 459 | 177; 512 from 2560 (96 blocks) 135 /
 // 124 | 184 | 123, from 2816 (104 blocks, whose 208 workgroups leave dQ too few CUs) 136 / 152 | 188 | 127, from 3500 145 / 198 | 205 | 146.
+//
+// With sinks the queries of a key fall into two: those of its window, the window kernel's as without sinks, and, for the sinks themselves, the
+// later ones.  SINKS_KEYS: the latter, `key_block` from the block of kv_first on; their sums are left for, or added to, the sinks' rows alone.  WINDOW_KEYS: the former; in
+// the place of keys before the first window another row is read, so that what was evicted between the sinks and the window may hold anything.
+enum DkvPart { ALL_KEYS, WINDOW_KEYS, SINKS_KEYS };
 constexpr int KV_STAGES = 4;
 constexpr int CHAIN = 6;                 // LDS fragments requested ahead of the products (dK/dV)
 
@@ -994,18 +1076,25 @@ struct DkvShared {
   float sL[KV_STAGES][QT];                        // (log2-domain) log-sum-exp of the tile's queries
   float sDl[KV_STAGES][QT];                       // delta of the tile's queries
 };
-template <int DH, bool IN_TURN>
+template <int DH, bool IN_TURN, DkvPart PART = ALL_KEYS>
 __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int bh, int slice, const bf16_t* __restrict__ q,
                                           const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o,
                                           const float* __restrict__ lse2, const float* __restrict__ delta, float* __restrict__ dk,
                                           float* __restrict__ dv, int Hq, int Hkv, int q_start, int c, float scale, int window, const AttnSeqs& seqs,
-                                          int key_block0, int slices, float* __restrict__ part) {
+                                          int key_block0, int slices, float* __restrict__ part, int sinks = 0) {
+  constexpr bool SINK = PART == SINKS_KEYS;
+  static_assert(!(IN_TURN && PART != ALL_KEYS), "with sinks, shares are taken with a break");
   const int sq = bh / Hkv, kvh = bh - sq * Hkv, kv_first = seqs.first[sq];
+  const int sink_end = kv_first + min(sinks, max(0, q_start + c - kv_first));
+  if (SINK) key_block0 = kv_first / KV_TILE;
+  // rows of the parts: first_part .. last_part - 1
+  const int first_part = SINK ? kv_first : key_block0 * KV_TILE, last_part = SINK ? sink_end : q_start + c;
+  const int64_t part_rows = SINK ? sinks : q_start + c - first_part;
   {
     const int64_t nq = (int64_t)sq * c * Hq, nk = (int64_t)sq * c * Hkv * DH;
     q += nq * DH; d_o += nq * DH; lse2 += 2 * nq; delta += 2 * nq;
     k += nk; v += nk; dk += nk; dv += nk;
-    if (part) part += (int64_t)sq * slices * 2 * (q_start + c - key_block0 * KV_TILE) * Hkv * DH;
+    if (part) part += (int64_t)sq * slices * 2 * part_rows * Hkv * DH;
   }
   auto& sQD = sh.sQD;
   auto& sP = sh.sP;
@@ -1021,6 +1110,12 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
   const int kw0 = key0 + kb * 32;      // a lane has the keys li and 16 + li from there on
   auto key_of = [&](int b) { return kw0 + b * 16 + li; };
   auto key_row = [&](int b) { return (int64_t)min(key_of(b), n_total - 1); };
+  auto read_row = [&](int b) {      // of K and V
+    int key = key_of(b);
+    if (SINK) key = max(min(key, sink_end - 1), kv_first);      // (a sink's, for keys that are none)
+    if (PART == WINDOW_KEYS) key = max(max(key, kv_first), q_start - min(window, n_total) + 1);
+    return (int64_t)min(key, n_total - 1);
+  };
   const int64_t kv_stride = (int64_t)Hkv * DH;
   const int64_t q_stride = (int64_t)Hq * DH;
 
@@ -1049,7 +1144,7 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
   bf16x8 breg[2][KS];   // B operand of the first product: K rows (role P) or V rows (role S) of my keys
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    const bf16_t* src = (role_p ? k : v) + key_row(b) * kv_stride + (int64_t)kvh * DH + lg * 8;
+    const bf16_t* src = (role_p ? k : v) + read_row(b) * kv_stride + (int64_t)kvh * DH + lg * 8;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) breg[b][kk] = *(const bf16x8*)(src + kk * 32);
   }
@@ -1062,10 +1157,12 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
 
   // query tiles that can see at least one key of this workgroup: query position >= key0
   // ... and, under a sliding window, query position <= last key of the workgroup + window - 1
-  const int qt_first = max(0, key0 - q_start) / QT;
+  // SINK: those of which some query has passed its window
+  const int past = SINK ? min(window, n_total) : 0;
+  const int qt_first = max(0, max(key0, SINK ? kv_first : 0) - q_start + past) / QT;
   int n_qt = (c + QT - 1) / QT;
-  if (window > 0) n_qt = min(n_qt, max(0, key0 + KV_TILE - 1 + window - 1 - q_start) / QT + 1);
-  const int n_all = key0 + KV_TILE <= kv_first ? 0 : max(0, n_qt - qt_first) * G;      // (a sequence of several may hide blocks that others see)
+  if (!SINK && window > 0) n_qt = min(n_qt, max(0, key0 + KV_TILE - 1 + window - 1 - q_start) / QT + 1);
+  const int n_all = key0 + KV_TILE <= kv_first || (SINK && key0 >= sink_end) ? 0 : max(0, n_qt - qt_first) * G;      // (a sequence of several may hide blocks that others see)
   auto share = [&](int z) { return (int)((int64_t)n_all * z / slices); };      // first step of share z
   for (int z = part ? slice : 0, z_last = IN_TURN ? 0 : part ? slice : slices - 1; z <= z_last; ++z) {
   const int it0 = IN_TURN ? 0 : share(z), n_iter = (IN_TURN ? n_all : share(z + 1)) - it0;
@@ -1088,6 +1185,7 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
   // One 64-query tile = two 32-query blocks.  `active`: the wave has a valid key and some query of the tile is
   // at or after its first key (the same answer for both waves of a key block).
   auto tile_active = [&](int qbase) {
+    if (SINK) return kw0 < sink_end && kw0 + 31 >= kv_first && q_start + min(qbase + QT, c) - 1 >= max(kw0, kv_first) + past;
     return kw0 < n_total && q_start + min(qbase + QT, c) - 1 >= kw0 && kw0 + 31 >= kv_first &&
            (window == 0 || q_start + qbase - window < kw0 + 31);     // the tile's first query still reaches the wave's last key
   };
@@ -1171,14 +1269,14 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
     auto vector = [&]() __attribute__((always_inline)) {
       const uint32_t stat = stat_lane + (uint32_t)(j % KV_STAGES) * QT * 4;
       if constexpr (RP) {
-        const bool diag = (q_start + qbase < kw0 + 31) || (qbase + QT > c) || kw0 < kv_first ||   // some pair masked, or ragged query tile
+        const bool diag = SINK || (q_start + qbase < kw0 + 31) || (qbase + QT > c) || kw0 < kv_first ||   // some pair masked, or ragged query tile
                           (window > 0 && q_start + qbase + QT - 1 - window >= kw0);
         if (diag) {
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             // query 4 lg + e of the tile sees the key for from <= e < from + n: one unsigned comparison
-            const int key = key_of(b), lo = max(0, key - q_start), hi = window > 0 ? min(c, key + min(window, n_total) - q_start) : c;
-            const uint32_t n = key < kv_first ? 0u : (uint32_t)max(0, hi - lo);
+            const int key = key_of(b), lo = max(0, key - q_start + past), hi = !SINK && window > 0 ? min(c, key + min(window, n_total) - q_start) : c;
+            const uint32_t n = key < kv_first || (SINK && key >= sink_end) ? 0u : (uint32_t)max(0, hi - lo);
             const int from = lo - qbase - 4 * lg;
 #pragma unroll
             for (int qb = 0; qb < 4; ++qb) {
@@ -1294,14 +1392,14 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
     if constexpr (IN_TURN) close();
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      if (key_of(b) >= n_total) continue;
+      if (key_of(b) >= last_part || (SINK && key_of(b) < kv_first)) continue;
       if constexpr (IN_TURN) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) *(f32x4*)(out_of(b) + d * 16) = sum[b][d];
       } else {
         // several workgroups per key block: each leaves its sum in its own slice [workgroup][dk | dv][key][kv head][DH]
-        const int64_t first = (int64_t)key_block0 * KV_TILE;
-        float* to = part ? part + ((int64_t)z * 2 + (RP ? 1 : 0)) * (n_total - first) * kv_stride + (key_of(b) - first) * kv_stride + (int64_t)kvh * DH + 4 * lg : out_of(b);
+        const int64_t first = first_part;
+        float* to = part ? part + ((int64_t)z * 2 + (RP ? 1 : 0)) * part_rows * kv_stride + (key_of(b) - first) * kv_stride + (int64_t)kvh * DH + 4 * lg : out_of(b);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
           f32x4 u = part ? f32x4{0.f, 0.f, 0.f, 0.f} : *(f32x4*)(to + d * 16);
@@ -1331,6 +1429,44 @@ __global__ __launch_bounds__(KV_THREADS) void attn_bwd_dkv_mfma_k(const bf16_t* 
   __shared__ __attribute__((aligned(1024))) DkvShared<DH> sh;
   dkv_block<DH, false>(sh, blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window,
                        seqs, key_block0, slices, part);
+}
+
+template <int DH>
+__global__ __launch_bounds__(KV_THREADS) void attn_bwd_dkv_window_k(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
+                                                                  const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o,
+                                                                  const float* __restrict__ lse2, const float* __restrict__ delta,
+                                                                  float* __restrict__ dk, float* __restrict__ dv, int Hq, int Hkv,
+                                                                  int q_start, int c, float scale, int window, const AttnSeqs seqs,
+                                                                  int key_block0, int slices, float* __restrict__ part) {
+  __shared__ __attribute__((aligned(1024))) DkvShared<DH> sh;
+  dkv_block<DH, false, WINDOW_KEYS>(sh, blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window,
+                       seqs, key_block0, slices, part);
+}
+// dK/dV of the sinks from the queries that have passed their window: blockIdx.x: 128-key block from that of kv_first on
+template <int DH>
+__global__ __launch_bounds__(KV_THREADS) void attn_bwd_dkv_sinks_k(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
+                                                                   const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o,
+                                                                   const float* __restrict__ lse2, const float* __restrict__ delta,
+                                                                   float* __restrict__ dk, float* __restrict__ dv, int Hq, int Hkv,
+                                                                   int q_start, int c, float scale, int window, const AttnSeqs seqs,
+                                                                   int slices, float* __restrict__ part, int sinks) {
+  __shared__ __attribute__((aligned(1024))) DkvShared<DH> sh;
+  dkv_block<DH, false, SINKS_KEYS>(sh, blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window,
+                             seqs, 0, slices, part, sinks);
+}
+// ... whose parts [sequence][slice][dk | dv][sink][kv head][DH] are added to dk / dv in their order (blockIdx.y: sequence), four elements a thread
+template <int DH>
+__global__ __launch_bounds__(256) void attn_sinks_sum_k(const float* __restrict__ part, int slices, int sinks, int Hkv, float* __restrict__ dk, float* __restrict__ dv,
+                                                        int n_total, const AttnSeqs seqs) {
+  const int64_t row = (int64_t)Hkv * DH, n = sinks * row, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;      // dk, then dv
+  if (i >= 2 * n) return;
+  const int64_t at = i < n ? i : i - n, key = seqs.first[blockIdx.y] + at / row;
+  if (key >= n_total) return;
+  float* out = (i < n ? dk : dv) + (blockIdx.y * (int64_t)n_total + key) * row + at % row;
+  const float* src = part + blockIdx.y * (int64_t)slices * 2 * n + i;
+  f32x4 x = *(const f32x4*)out;
+  for (int z = 0; z < slices; ++z) x += *(const f32x4*)(src + z * 2 * n);
+  *(f32x4*)out = x;
 }
 
 // dK/dV and dQ in one launch, the longer workgroups first: for chunks that are a few rounds of the chip, where each
@@ -1462,11 +1598,15 @@ template <int DH>
 static hipError_t forward_dh(const AttnArgs& a, hipStream_t st) {
   if (a.q_len == 0) return hipSuccess;
   const int64_t heads = (int64_t)a.Hq * a.batch, full = cdiv(a.q_len, TQ) * heads, halves = cdiv(a.q_len, TQ / 2) * heads;
-  auto launch = [&](auto kernel, int64_t n) {
+  auto launch = [&](auto kernel, int64_t n, auto... more) {
     kernel<<<(unsigned)n, AT_THREADS, 0, st>>>((bf16_t*)a.q, (const bf16_t*)a.k, (const bf16_t*)a.v, (bf16_t*)a.o, a.lse, a.Hq, a.Hkv,
-                                               a.q_start, a.q_len, a.scale, a.rope_q, a.window, sequences(a));
+                                               a.q_start, a.q_len, a.scale, a.rope_q, a.window, sequences(a), more...);
   };
-  if (attn_half_tiles_faster(a, attn_half_step_forward(DH))) launch(attn_fwd_mfma_k<DH, true>, halves);
+  const bool half = attn_half_tiles_faster(a, attn_half_step_forward(DH));
+  if (a.sinks > 0) {
+    if (half) launch(attn_fwd_sinks_k<DH, true>, halves, a.sinks);
+    else launch(attn_fwd_sinks_k<DH, false>, full, a.sinks);
+  } else if (half) launch(attn_fwd_mfma_k<DH, true>, halves);
   else launch(attn_fwd_mfma_k<DH, false>, full);
   return hipGetLastError();
 }
@@ -1483,6 +1623,15 @@ static hipError_t backward_dh(const AttnArgs& a, hipStream_t st) {
   const int slices = std::max(1, a.dkv_slices);
   float* part = p.parts ? a.dkv_scratch : nullptr;
   const bf16_t *q = (const bf16_t*)a.q, *k = (const bf16_t*)a.k, *v = (const bf16_t*)a.v, *d_o = (const bf16_t*)a.d_o;
+  if (a.sinks > 0) {
+    if (const int blocks = attn_sink_blocks(a)) {      // before the others: what their sums add is what the chunk's own rows leave with
+      float* sums = a.sink_slices > 1 ? a.dkv_scratch : nullptr;
+      attn_bwd_dkv_sinks_k<DH><<<dim3((unsigned)blocks, a.Hkv * a.batch, sums ? (unsigned)a.sink_slices : 1u), KV_THREADS, 0, st>>>(
+          q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, a.sink_slices, sums, a.sinks);
+      if (sums)
+        attn_sinks_sum_k<DH><<<dim3((unsigned)cdiv((int64_t)2 * a.sinks * a.Hkv * DH, 1024), a.batch), 256, 0, st>>>(sums, a.sink_slices, a.sinks, a.Hkv, a.dk, a.dv, a.q_start + a.q_len, seqs);
+    }
+  }
   if (p.one_launch) {
     auto launch = [&](auto kernel) {
       kernel<<<(unsigned)(p.n_dkv + p.n_dq), AT_THREADS, 0, st>>>(q, k, v, d_o, a.lse, lse2, a.delta, (bf16_t*)a.dq, a.dk, a.dv, a.Hq, a.Hkv, a.q_start,
@@ -1494,15 +1643,23 @@ static hipError_t backward_dh(const AttnArgs& a, hipStream_t st) {
     else if (p.halves) launch(attn_bwd_mfma_k<DH, true>);
     else launch(attn_bwd_mfma_k<DH, false>);
   } else {
-    auto launch_dq = [&](auto kernel) {
+    auto launch_dq = [&](auto kernel, auto... more) {
       kernel<<<(unsigned)p.n_dq, AT_THREADS, 0, st>>>(q, k, v, d_o, a.lse, a.delta, (bf16_t*)a.dq, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale,
-                                                                    a.rope_q, a.window, seqs, p.q_blocks);
+                                                                    a.rope_q, a.window, seqs, p.q_blocks, more...);
     };
-    if (p.halves) launch_dq(attn_bwd_dq_mfma_k<DH, true>);
+    if (a.sinks > 0) {
+      if (p.halves) launch_dq(attn_bwd_dq_sinks_k<DH, true>, a.sinks);
+      else launch_dq(attn_bwd_dq_sinks_k<DH, false>, a.sinks);
+    } else if (p.halves) launch_dq(attn_bwd_dq_mfma_k<DH, true>);
     else launch_dq(attn_bwd_dq_mfma_k<DH, false>);
-    if (p.n_dkv > 0)
-      attn_bwd_dkv_mfma_k<DH><<<dim3((unsigned)p.key_blocks, a.Hkv * a.batch, part ? (unsigned)slices : 1u), KV_THREADS, 0, st>>>(
+    auto launch_dkv = [&](auto kernel) {
+      kernel<<<dim3((unsigned)p.key_blocks, a.Hkv * a.batch, part ? (unsigned)slices : 1u), KV_THREADS, 0, st>>>(
           q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, p.key_block0, slices, part);
+    };
+    if (p.n_dkv > 0) {
+      if (a.sinks > 0) launch_dkv(attn_bwd_dkv_window_k<DH>);
+      else launch_dkv(attn_bwd_dkv_mfma_k<DH>);
+    }
   }
   if (part) {
     const int first = p.key_block0 * KV_TILE;

@@ -14,7 +14,7 @@ inline double attn_launch_steps(const AttnArgs& a, int tile, int keys) {
   auto steps_of = [&](int64_t row) {
     const int64_t first_q = a.q_start + row * tile, last = std::min<int64_t>(a.q_start + a.q_len, first_q + tile);
     const int64_t first = std::max<int64_t>(a.kv_first, a.window > 0 ? first_q - a.window + 1 : 0);
-    return cdiv(std::max<int64_t>(last - first, 0), keys) + 6;
+    return cdiv(std::max<int64_t>(last - first, 0) + std::min<int64_t>(a.sinks, first - a.kv_first), keys) + 6;
   };
   if (rows * heads > 8 * 256) {
     double sum = 0.0;
@@ -76,7 +76,7 @@ inline AttnBackwardPlan attn_backward_plan(const AttnArgs& a, int most, int most
   const int slices = std::max(1, a.dkv_slices), tile = p.halves ? ATTN_TILE_Q / 2 : ATTN_TILE_Q;
   const int64_t blocks = (int64_t)p.key_blocks * a.Hkv * a.batch;
   p.parts = slices > 1 && a.dkv_scratch;
-  p.in_turn = slices > 1 && !p.parts && blocks > 0 && blocks <= ATTN_IN_TURN_BLOCKS;
+  p.in_turn = a.sinks == 0 && slices > 1 && !p.parts && blocks > 0 && blocks <= ATTN_IN_TURN_BLOCKS;
   p.n_dkv = blocks * (p.in_turn ? 2 : p.parts ? slices : 1);
   p.q_blocks = (int)cdiv(a.q_len, tile);
   p.n_dq = (int64_t)p.q_blocks * a.Hq * a.batch;
@@ -93,7 +93,7 @@ inline AttnBackwardPlan attn_backward_plan(const AttnArgs& a, int most, int most
   const int64_t dkv_steps = cdiv(seen_by, ATTN_KV_QUERIES) * (a.Hq / a.Hkv) / (p.parts ? slices : 1);
   p.dq_first = dq_steps > dkv_steps && p.n_dq <= ATTN_DQ_FIRST;
   const int64_t n = p.n_dkv + p.n_dq;
-  p.one_launch = p.n_dkv > 0 && (p.in_turn || (p.dq_first && a.q_start > 0) || n <= (a.q_start > 0 ? most_prefix : most));
+  p.one_launch = a.sinks == 0 && p.n_dkv > 0 && (p.in_turn || (p.dq_first && a.q_start > 0) || n <= (a.q_start > 0 ? most_prefix : most));
   // Workgroup b runs on XCD b % 8.  With the key blocks side by side an XCD has every eighth of them: where the chunk's own blocks, which ever fewer queries see, are
   // many, up to 2.4 times the work of another (2048 queries from 0, 28 / 4 heads 182 us, the heads of a block side by side 133, from 2048 344 / 328; 32 / 8 heads
   // 385 / 352 from 0, 790 / 769 from 6144).  Where they are an eighth or less, or each workgroup has a CU of its own, there is nothing to even out, and a head's

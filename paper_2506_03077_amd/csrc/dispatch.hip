@@ -76,8 +76,8 @@ static double causal_pairs(const AttnArgs& a) {   // visible (query, key) pairs 
   double pairs = 0.0;
   for (int b = 0; b < a.batch; ++b)
     for (int t = 0; t < a.q_len; ++t) {
-      const int p = a.q_start + t, lo = std::max(a.kv_firsts ? a.kv_firsts[b] : a.kv_first, a.window > 0 ? p - a.window + 1 : 0);
-      pairs += std::max(0, p - lo + 1);
+      const int p = a.q_start + t, first = a.kv_firsts ? a.kv_firsts[b] : a.kv_first, lo = std::max(first, a.window > 0 ? p - a.window + 1 : 0);
+      pairs += std::max(0, p - lo + 1) + (p >= first ? std::min(a.sinks, lo - first) : 0);
     }
   return (double)a.Hq * pairs;
 }

@@ -4,6 +4,8 @@
 #pragma once
 #include "common.h"
 
+#include <algorithm>
+
 namespace sbp {
 
 // C[M,N] (=|+=) sum_k A(m,k) * B(k,n), fp32 accumulation.
@@ -177,6 +179,7 @@ struct AttnArgs {
   float scale;
   int window = 0;          // > 0: a query at position t sees only keys t - window < u <= t
   int kv_first = 0;        // key positions before this one are padding: never visible
+  int sinks = 0;           // the first `sinks` keys from kv_first on stay visible to every later query; 0 without a window, at most all keys (attn_set_sinks)
   // Several sequences in one call, up to ATTN_MAX_SEQS: `batch` of q_len queries and keys each, one behind the other (q_start = 0; lse [batch, Hq, c],
   // delta [batch, 2, Hq, c]), kv_firsts their kv_first on the host (or NULL: kv_first for all; else kv_first is the least of them).
   int batch = 1;
@@ -189,6 +192,7 @@ struct AttnArgs {
   // attn_dkv_scratch_bytes) that lets a workgroup take each
   int dkv_slices = 1;
   float* dkv_scratch = nullptr;
+  int sink_slices = 1;     // ... that the queries past a sink's window are cut into (attn_sink_slices); their sums meet in the same scratch
   // Optional rotary embedding of the chunk's queries folded into the attention kernels: cos/sin rows [c, dh/2] of the
   // chunk's positions.  Forward: q arrives un-rotated, is rotated on load and written back rotated (q must then be
   // writable); backward: q is the rotated tensor the forward left, and dq leaves the kernel already rotated back
@@ -237,6 +241,28 @@ inline int attn_dkv_slices(const AttnArgs& a, size_t max_bytes) {
     if (s == 1 || cost < best_cost) { best = s; best_cost = cost; }
   }
   return best;
+}
+
+// dK/dV of the sinks from the queries past their window: key blocks of a sequence (0: no query is), and the slices of their walk, a workgroup each: as many as
+// give every CU one, of four steps at least.  Like the others a property of the sizes.
+inline int attn_sink_blocks(const AttnArgs& a) {
+  if (a.sinks == 0 || (int64_t)a.q_start + a.q_len - 1 < (int64_t)a.kv_first + a.window) return 0;
+  return (int)cdiv((a.kv_firsts ? ATTN_KV_TILE - 1 : a.kv_first % ATTN_KV_TILE) + (int64_t)a.sinks, ATTN_KV_TILE);
+}
+inline size_t attn_sink_scratch_bytes(const AttnArgs& a, int slices) {      // [sequence][slice][dk | dv][sink][kv head][dh] fp32
+  return slices < 2 ? 0 : (size_t)a.batch * slices * 2 * a.sinks * a.Hkv * a.dh * sizeof(float);
+}
+inline int attn_sink_slices(const AttnArgs& a, size_t max_bytes) {
+  const int64_t blocks = (int64_t)attn_sink_blocks(a) * a.Hkv * a.batch;
+  if (blocks == 0) return 1;
+  const int64_t steps = cdiv(std::min<int64_t>(a.q_len, (int64_t)a.q_start + a.q_len - a.kv_first - a.window), ATTN_KV_QUERIES) * (a.Hq / a.Hkv);
+  int64_t s = std::max<int64_t>(1, std::min<int64_t>(256 / blocks, steps / 4));
+  while (s > 1 && attn_sink_scratch_bytes(a, (int)s) > max_bytes) --s;
+  return (int)s;
+}
+// what a caller's `sinks` come to
+inline void attn_set_sinks(AttnArgs& a, int sinks) {
+  a.sinks = a.window > 0 ? (int)std::min<int64_t>(sinks, std::max<int64_t>(0, (int64_t)a.q_start + a.q_len - a.kv_first)) : 0;
 }
 
 // ---- LM head rows ----
