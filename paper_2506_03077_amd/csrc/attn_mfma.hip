@@ -1064,7 +1064,14 @@ __global__ __launch_bounds__(AT_THREADS) void attn_bwd_dq_sinks_k(const bf16_t* 
 // With sinks the queries of a key fall into two: those of its window, the window kernel's as without sinks, and, for the sinks themselves, the
 // later ones.  SINKS_KEYS: the latter, `key_block` from the block of kv_first on; their sums are left for, or added to, the sinks' rows alone.  WINDOW_KEYS: the former; in
 // the place of keys before the first window another row is read, so that what was evicted between the sinks and the window may hold anything.
+// Both hand P over as fp16 where ALL_KEYS has bf16 (heads of 128), 2^15 P, the largest of which fp16 holds, so that the smallest that counts does not leave its normal range;
+// the exponent, a power of two, costs nothing and leaves with the last factor.  dS is then rounded to bf16 once instead of twice: error of dk against fp64 2.4e-3
+// instead of 2.9e-3, of which its own rounding to bf16 is 1.7e-3.
 enum DkvPart { ALL_KEYS, WINDOW_KEYS, SINKS_KEYS };
+constexpr float P16_LOG2 = 15.f;
+template <int DH> constexpr bool P16_HEADS = !FP32_STATS<DH>;
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 constexpr int KV_STAGES = 4;
 constexpr int CHAIN = 6;                 // LDS fragments requested ahead of the products (dK/dV)
 
@@ -1082,7 +1089,7 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
                                           const float* __restrict__ lse2, const float* __restrict__ delta, float* __restrict__ dk,
                                           float* __restrict__ dv, int Hq, int Hkv, int q_start, int c, float scale, int window, const AttnSeqs& seqs,
                                           int key_block0, int slices, float* __restrict__ part, int sinks = 0) {
-  constexpr bool SINK = PART == SINKS_KEYS;
+  constexpr bool SINK = PART == SINKS_KEYS, P16 = PART != ALL_KEYS && P16_HEADS<DH>;
   static_assert(!(IN_TURN && PART != ALL_KEYS), "with sinks, shares are taken with a break");
   const int sq = bh / Hkv, kvh = bh - sq * Hkv, kv_first = seqs.first[sq];
   const int sink_end = kv_first + min(sinks, max(0, q_start + c - kv_first));
@@ -1202,7 +1209,7 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int d = 0; d < DB; ++d) acc[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float f = RP ? 1.0f : scale;
+    const float f = (RP ? 1.0f : scale) * (P16 ? 0x1p-15f : 1.0f);
     int present = 0, present_end = IN_TURN ? share(1) : 0;      // IN_TURN: the share that is being summed, and the step after it
     auto close = [&]() __attribute__((always_inline)) {         // total += the share's sum
 #pragma unroll
@@ -1301,7 +1308,16 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             terms(b, ks);
-            if constexpr (!FP32_STATS<DH>)
+            if constexpr (P16) {
+              half8 h;
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) {
+                const half2v x = __builtin_convertvector((f32x2{t[b][2 * ks + (e >> 2)][e & 3], t[b][2 * ks + (e >> 2)][(e & 3) + 1]}), half2v);
+                h[e] = x[0];
+                h[e + 1] = x[1];
+              }
+              *(half8*)(__attribute__((address_space(3))) char*)(uintptr_t)(sp_lane + (b * 2 + ks) * 1024) = h;
+            } else if constexpr (!FP32_STATS<DH>)
               *(bf16x8*)(__attribute__((address_space(3))) char*)(uintptr_t)(sp_lane + (b * 2 + ks) * 1024) = w[0][b][ks];
             else {
 #pragma unroll
@@ -1322,6 +1338,10 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
             if constexpr (FP32_STATS<DH>) {
               const float4 p0 = lds_f4(sp_lane + (b * 4 + 2 * ks) * 1024), p1 = lds_f4(sp_lane + (b * 4 + 2 * ks + 1) * 1024);
               pv[0] = p0.x; pv[1] = p0.y; pv[2] = p0.z; pv[3] = p0.w; pv[4] = p1.x; pv[5] = p1.y; pv[6] = p1.z; pv[7] = p1.w;
+            } else if constexpr (P16) {
+              const half8 p8 = __builtin_bit_cast(half8, lds_b128(sp_lane + (b * 2 + ks) * 1024));
+#pragma unroll
+              for (int e = 0; e < 8; ++e) pv[e] = (float)p8[e];
             } else {
               const bf16x8 p8 = lds_b128(sp_lane + (b * 2 + ks) * 1024);
 #pragma unroll
@@ -1454,21 +1474,6 @@ __global__ __launch_bounds__(KV_THREADS) void attn_bwd_dkv_sinks_k(const bf16_t*
   dkv_block<DH, false, SINKS_KEYS>(sh, blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window,
                              seqs, 0, slices, part, sinks);
 }
-// ... whose parts [sequence][slice][dk | dv][sink][kv head][DH] are added to dk / dv in their order (blockIdx.y: sequence), four elements a thread
-template <int DH>
-__global__ __launch_bounds__(256) void attn_sinks_sum_k(const float* __restrict__ part, int slices, int sinks, int Hkv, float* __restrict__ dk, float* __restrict__ dv,
-                                                        int n_total, const AttnSeqs seqs) {
-  const int64_t row = (int64_t)Hkv * DH, n = sinks * row, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;      // dk, then dv
-  if (i >= 2 * n) return;
-  const int64_t at = i < n ? i : i - n, key = seqs.first[blockIdx.y] + at / row;
-  if (key >= n_total) return;
-  float* out = (i < n ? dk : dv) + (blockIdx.y * (int64_t)n_total + key) * row + at % row;
-  const float* src = part + blockIdx.y * (int64_t)slices * 2 * n + i;
-  f32x4 x = *(const f32x4*)out;
-  for (int z = 0; z < slices; ++z) x += *(const f32x4*)(src + z * 2 * n);
-  *(f32x4*)out = x;
-}
-
 // dK/dV and dQ in one launch, the longer workgroups first: for chunks that are a few rounds of the chip, where each
 // launch on its own leaves CUs idle at its end (AttnBackwardPlan).
 template <int DH, bool SPLIT, bool IN_TURN>
@@ -1501,6 +1506,32 @@ __device__ __forceinline__ void bwd_block(const bf16_t* __restrict__ q, const bf
 #define BWD_ARGS q, k, v, d_o, lse, lse2, delta, dq, dk, dv, Hq, Hkv, q_start, c, scale, rope, window, seqs, key_block0, key_blocks, slices, part, q_blocks, dq_first, side_by_side
 template <int DH, bool SPLIT> __global__ __launch_bounds__(AT_THREADS) void attn_bwd_mfma_k(BWD_PARAMS) { bwd_block<DH, SPLIT, false>(BWD_ARGS); }
 template <int DH, bool SPLIT> __global__ __launch_bounds__(AT_THREADS) void attn_bwd_in_turn_k(BWD_PARAMS) { bwd_block<DH, SPLIT, true>(BWD_ARGS); }
+// ... and with sinks: their shares come last, the shortest workgroups.  They need room for their sums, as the workgroups of the windows add to the same rows.
+template <int DH, bool SPLIT>
+__global__ __launch_bounds__(AT_THREADS) void attn_bwd_sinks_k(BWD_PARAMS, int sinks, int sink_blocks, int sink_slices, float *__restrict__ sink_part) {
+  __shared__ __attribute__((aligned(1024))) union { DkvShared<DH> dkv; DqShared<DH, SPLIT> dq; } sh;
+  const int kv_heads = Hkv * seqs.n, heads = Hq * seqs.n, n_dkv = key_blocks * kv_heads * (part ? slices : 1), n_dq = q_blocks * heads;
+  int b = (int)blockIdx.x;
+  if (b >= n_dkv + n_dq) {
+    b -= n_dkv + n_dq;
+    const int block = b % sink_blocks, r = b / sink_blocks;
+    dkv_block<DH, false, SINKS_KEYS>(sh.dkv, block, r % kv_heads, r / kv_heads, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window, seqs, 0,
+                                     sink_slices, sink_part, sinks);
+    return;
+  }
+  if (dq_first) b = b < n_dq ? b + n_dkv : b - n_dq;
+  if (b < n_dkv) {
+    const int of = side_by_side ? key_blocks : n_dkv / key_blocks, slow = __builtin_amdgcn_readfirstlane(b / of), fast = b - slow * of;
+    const int r = side_by_side ? slow : fast;
+    dkv_block<DH, false, WINDOW_KEYS>(sh.dkv, side_by_side ? fast : slow, r % kv_heads, r / kv_heads, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale,
+                                      window, seqs, key_block0, slices, part);
+  } else {
+    const int i = b - n_dkv;
+    int qt = q_blocks - 1 - i / heads, bh = i % heads;
+    if (q_blocks * heads > 256) query_tile_of(i, q_blocks, heads, qt, bh);
+    dq_tile<DH, SPLIT, true>(sh.dq, qt, bh, q, k, v, d_o, lse, delta, dq, Hq, Hkv, q_start, c, scale, rope, window, seqs, sinks);
+  }
+}
 #undef BWD_PARAMS
 #undef BWD_ARGS
 
@@ -1545,13 +1576,63 @@ __global__ __launch_bounds__(256) void attn_dkv_sum_k(const float* __restrict__ 
   *(bf16x4*)(fin + DH / 2) = w;
 }
 
+// The same of a call with sinks: after the parts of the windows (or NULL) those of the sinks, [sequence][slice][dk | dv][sink][kv head][DH] (or NULL).  Rows of a
+// sequence: with parts of the windows, the sinks before `first` and the keys from there on, else the sinks; at most max_rows.
+template <int DH>
+__global__ __launch_bounds__(256) void attn_dkv_sum_sinks_k(const float* __restrict__ part, int slices, int first, const float* __restrict__ sink_part, int sink_slices,
+                                                            int sinks, int64_t max_rows, int Hkv, float* __restrict__ dk, float* __restrict__ dv, int q_start, int n_total,
+                                                            bf16_t* __restrict__ dkc, bf16_t* __restrict__ dvc, const float2* __restrict__ rope, const AttnSeqs seqs) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = max_rows * Hkv * (DH / 8), sq = blockIdx.y;      // dk, then dv
+  if (i >= 2 * all) return;
+  const int kv_first = seqs.first[sq], sink_end = kv_first + min(sinks, max(0, n_total - kv_first));
+  const bool is_dk = i < all;
+  const int64_t p = is_dk ? i : i - all, rh = p / (DH / 8);
+  const int r = (int)(rh / Hkv), head = (int)(rh % Hkv), e = (int)(p % (DH / 8)) * 4;
+  const int before = part ? max(0, min(first, sink_end) - kv_first) : sink_end - kv_first;      // rows that come as sinks
+  if (r >= before && !part) return;
+  const int key = r < before ? kv_first + r : first + r - before;
+  if (key >= n_total) return;
+  const int64_t row = (int64_t)Hkv * DH, at = head * DH + e;
+  float* out = (is_dk ? dk : dv) + (sq * n_total + key) * row + at;
+  f32x4 x = *(const f32x4*)out, y = *(const f32x4*)(out + DH / 2);
+  auto add = [&](const float* src, int n, int64_t step) {
+#pragma unroll 4
+    for (int z = 0; z < n; ++z) {
+      x += *(const f32x4*)(src + z * step);
+      y += *(const f32x4*)(src + z * step + DH / 2);
+    }
+  };
+  if (part && key >= first) {
+    const int64_t n = (n_total - first) * row;
+    add(part + sq * slices * 2 * n + (is_dk ? 0 : n) + (key - first) * row + at, slices, 2 * n);
+  }
+  if (sink_part && key >= kv_first && key < sink_end) {
+    const int64_t n = sinks * row;
+    add(sink_part + sq * sink_slices * 2 * n + (is_dk ? 0 : n) + (key - kv_first) * row + at, sink_slices, 2 * n);
+  }
+  *(f32x4*)out = x;
+  *(f32x4*)(out + DH / 2) = y;
+  const int64_t own = (int64_t)key - q_start;
+  if (!dkc || own < 0) return;
+  bf16x4 u, w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 cs = is_dk ? rope[own * (DH / 2) + e + j] : make_float2(1.f, 0.f);
+    u[j] = (bf16_t)(is_dk ? x[j] * cs.x + y[j] * cs.y : x[j]);    // rotation by the negative angle
+    w[j] = (bf16_t)(is_dk ? y[j] * cs.x - x[j] * cs.y : y[j]);
+  }
+  bf16_t* fin = (is_dk ? dkc : dvc) + (sq * (n_total - q_start) + own) * row + at;
+  *(bf16x4*)fin = u;
+  *(bf16x4*)(fin + DH / 2) = w;
+}
+
 // delta[h, t] = sum_j d_o[t,h,j] * o[t,h,j]  (DH / 8 lanes per (t, h), 16 bytes of each tensor per lane)
 // also lse2[h, t] = lse[h, t] * log2(e), the form the dK/dV kernel's exp2 wants (one multiply per (t, h) here
 // instead of one per score there); 64-wide heads, whose exponents are natural differences: lse[h, t] itself
-template <int DH>
-__global__ __launch_bounds__(256) void attn_delta_mfma_k(const bf16_t* __restrict__ o, const bf16_t* __restrict__ d_o,
-                                                         const float* __restrict__ lse, float* __restrict__ delta,
-                                                         int Hq, int c) {
+// P16: less P16_LOG2 (see DkvPart)
+template <int DH, bool P16>
+__device__ __forceinline__ void delta_block(const bf16_t* __restrict__ o, const bf16_t* __restrict__ d_o, const float* __restrict__ lse,
+                                            float* __restrict__ delta, int Hq, int c) {
   constexpr int LANES = DH / 8;
   const int64_t first = (int64_t)blockIdx.y * c * Hq;      // blockIdx.y: sequence
   const int64_t pair = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;      // t * Hq + h
@@ -1569,8 +1650,18 @@ __global__ __launch_bounds__(256) void attn_delta_mfma_k(const bf16_t* __restric
     const int t = (int)(pair / Hq), h = (int)(pair % Hq);
     delta[(int64_t)h * c + t] = s;
     const float l = lse[(int64_t)h * c + t];
-    lse2[(int64_t)h * c + t] = l == -INFINITY ? 0.0f : FP32_STATS<DH> ? l : l * LOG2E;   // a query that saw no key: its scores are all masked anyway
+    lse2[(int64_t)h * c + t] = l == -INFINITY ? 0.0f : FP32_STATS<DH> ? l : P16 ? l * LOG2E - P16_LOG2 : l * LOG2E;   // a query that saw no key: its scores are all masked anyway
   }
+}
+template <int DH>
+__global__ __launch_bounds__(256) void attn_delta_mfma_k(const bf16_t* __restrict__ o, const bf16_t* __restrict__ d_o, const float* __restrict__ lse,
+                                                         float* __restrict__ delta, int Hq, int c) {
+  delta_block<DH, false>(o, d_o, lse, delta, Hq, c);
+}
+template <int DH>
+__global__ __launch_bounds__(256) void attn_delta_sinks_k(const bf16_t* __restrict__ o, const bf16_t* __restrict__ d_o, const float* __restrict__ lse,
+                                                          float* __restrict__ delta, int Hq, int c) {
+  delta_block<DH, P16_HEADS<DH>>(o, d_o, lse, delta, Hq, c);
 }
 
 bool attn_mfma_eligible(int dt, int dh, int Hq, int Hkv) { return dt == DT_BF16 && (dh == 128 || dh == 64) && Hq % Hkv == 0; }
@@ -1579,7 +1670,7 @@ static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // the MFMA kernels move 16 bytes per lane: every tensor they touch must be 16-byte aligned
 bool attn_mfma_aligned(const AttnArgs& a, bool backward) {
-  if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.o) || !aligned16(a.dkv_scratch) || ((uintptr_t)a.rope_q & 7)) return false;
+  if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.o) || !aligned16(a.dkv_scratch) || !aligned16(a.sink_scratch) || ((uintptr_t)a.rope_q & 7)) return false;
   return !backward || (aligned16(a.d_o) && aligned16(a.dq) && aligned16(a.dk) && aligned16(a.dv) && aligned16(a.dkc) && aligned16(a.dvc));
 }
 
@@ -1611,6 +1702,17 @@ static hipError_t forward_dh(const AttnArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// dkc and dvc of the chunk's own rows, from dk and dv
+template <int DH>
+static hipError_t own_rows_finish(const AttnArgs& a, hipStream_t st) {
+  hipError_t e = hipGetLastError();
+  const int64_t own = (int64_t)a.q_len * a.Hkv * DH, keys = own + (int64_t)a.q_start * a.Hkv * DH;      // elements of a sequence's rows of the chunk, of all its keys
+  for (int b = 0; b < a.batch && e == hipSuccess; ++b)
+    e = kv_grad_finish(a.dt, a.dk + b * keys + (keys - own), a.dv + b * keys + (keys - own), a.rope_k, (bf16_t*)a.dkc + b * own, (bf16_t*)a.dvc + b * own, a.q_len, a.Hkv,
+                       DH, st);
+  return e;
+}
+
 template <int DH>
 static hipError_t backward_dh(const AttnArgs& a, hipStream_t st) {
   if (a.q_len == 0) return hipSuccess;
@@ -1623,15 +1725,6 @@ static hipError_t backward_dh(const AttnArgs& a, hipStream_t st) {
   const int slices = std::max(1, a.dkv_slices);
   float* part = p.parts ? a.dkv_scratch : nullptr;
   const bf16_t *q = (const bf16_t*)a.q, *k = (const bf16_t*)a.k, *v = (const bf16_t*)a.v, *d_o = (const bf16_t*)a.d_o;
-  if (a.sinks > 0) {
-    if (const int blocks = attn_sink_blocks(a)) {      // before the others: what their sums add is what the chunk's own rows leave with
-      float* sums = a.sink_slices > 1 ? a.dkv_scratch : nullptr;
-      attn_bwd_dkv_sinks_k<DH><<<dim3((unsigned)blocks, a.Hkv * a.batch, sums ? (unsigned)a.sink_slices : 1u), KV_THREADS, 0, st>>>(
-          q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, a.sink_slices, sums, a.sinks);
-      if (sums)
-        attn_sinks_sum_k<DH><<<dim3((unsigned)cdiv((int64_t)2 * a.sinks * a.Hkv * DH, 1024), a.batch), 256, 0, st>>>(sums, a.sink_slices, a.sinks, a.Hkv, a.dk, a.dv, a.q_start + a.q_len, seqs);
-    }
-  }
   if (p.one_launch) {
     auto launch = [&](auto kernel) {
       kernel<<<(unsigned)(p.n_dkv + p.n_dq), AT_THREADS, 0, st>>>(q, k, v, d_o, a.lse, lse2, a.delta, (bf16_t*)a.dq, a.dk, a.dv, a.Hq, a.Hkv, a.q_start,
@@ -1643,23 +1736,15 @@ static hipError_t backward_dh(const AttnArgs& a, hipStream_t st) {
     else if (p.halves) launch(attn_bwd_mfma_k<DH, true>);
     else launch(attn_bwd_mfma_k<DH, false>);
   } else {
-    auto launch_dq = [&](auto kernel, auto... more) {
+    auto launch_dq = [&](auto kernel) {
       kernel<<<(unsigned)p.n_dq, AT_THREADS, 0, st>>>(q, k, v, d_o, a.lse, a.delta, (bf16_t*)a.dq, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale,
-                                                                    a.rope_q, a.window, seqs, p.q_blocks, more...);
+                                                                    a.rope_q, a.window, seqs, p.q_blocks);
     };
-    if (a.sinks > 0) {
-      if (p.halves) launch_dq(attn_bwd_dq_sinks_k<DH, true>, a.sinks);
-      else launch_dq(attn_bwd_dq_sinks_k<DH, false>, a.sinks);
-    } else if (p.halves) launch_dq(attn_bwd_dq_mfma_k<DH, true>);
+    if (p.halves) launch_dq(attn_bwd_dq_mfma_k<DH, true>);
     else launch_dq(attn_bwd_dq_mfma_k<DH, false>);
-    auto launch_dkv = [&](auto kernel) {
-      kernel<<<dim3((unsigned)p.key_blocks, a.Hkv * a.batch, part ? (unsigned)slices : 1u), KV_THREADS, 0, st>>>(
+    if (p.n_dkv > 0)
+      attn_bwd_dkv_mfma_k<DH><<<dim3((unsigned)p.key_blocks, a.Hkv * a.batch, part ? (unsigned)slices : 1u), KV_THREADS, 0, st>>>(
           q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, p.key_block0, slices, part);
-    };
-    if (p.n_dkv > 0) {
-      if (a.sinks > 0) launch_dkv(attn_bwd_dkv_window_k<DH>);
-      else launch_dkv(attn_bwd_dkv_mfma_k<DH>);
-    }
   }
   if (part) {
     const int first = p.key_block0 * KV_TILE;
@@ -1668,18 +1753,63 @@ static hipError_t backward_dh(const AttnArgs& a, hipStream_t st) {
                                                                        a.rope_k);
     if (first <= a.q_start) return hipGetLastError();
   }
-  if (a.dkc) {      // (also where some of the chunk's own keys, all hidden, come before the first visible block)
-    hipError_t e = hipGetLastError();
-    const int64_t own = (int64_t)a.q_len * a.Hkv * DH, keys = own + (int64_t)a.q_start * a.Hkv * DH;      // elements of a sequence's rows of the chunk, of all its keys
-    for (int b = 0; b < a.batch && e == hipSuccess; ++b)
-      e = kv_grad_finish(a.dt, a.dk + b * keys + (keys - own), a.dv + b * keys + (keys - own), a.rope_k, (bf16_t*)a.dkc + b * own, (bf16_t*)a.dvc + b * own, a.q_len, a.Hkv,
-                         DH, st);
-    return e;
+  if (a.dkc) return own_rows_finish<DH>(a, st);      // (also where some of the chunk's own keys, all hidden, come before the first visible block)
+  return hipGetLastError();
+}
+// With sinks.  dk and dv grow by the windows' share first, then by the sinks' (attn_dkv_sum_sinks_k, or launch after launch).
+template <int DH>
+static hipError_t backward_sinks(const AttnArgs& a, hipStream_t st) {
+  if (a.q_len == 0) return hipSuccess;
+  const int64_t pairs = (int64_t)a.q_len * a.Hq;
+  const float* lse2 = a.delta + pairs;
+  const AttnSeqs seqs = sequences(a);
+  attn_delta_sinks_k<DH><<<dim3((unsigned)cdiv(pairs, 256 / (DH / 8)), a.batch), 256, 0, st>>>((const bf16_t*)a.o, (const bf16_t*)a.d_o, a.lse, a.delta, a.Hq, a.q_len);
+  const AttnBackwardPlan p = attn_backward_plan(a, MERGED_MAX, MERGED_MAX_PREFIX);
+  const int slices = std::max(1, a.dkv_slices), n_total = a.q_start + a.q_len;
+  float *part = p.parts ? a.dkv_scratch : nullptr, *sink_part = p.sink_parts ? a.sink_scratch : nullptr;
+  const bf16_t *q = (const bf16_t*)a.q, *k = (const bf16_t*)a.k, *v = (const bf16_t*)a.v, *d_o = (const bf16_t*)a.d_o;
+  auto launch_sinks = [&](unsigned workgroups) {      // of a key block
+    attn_bwd_dkv_sinks_k<DH><<<dim3((unsigned)p.sink_blocks, a.Hkv * a.batch, workgroups), KV_THREADS, 0, st>>>(
+        q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, a.sink_slices, sink_part, a.sinks);
+  };
+  const bool in_place = p.sink_blocks > 0 && !sink_part;      // the sinks' shares one after the other, added where they belong once the windows' are
+  if (p.one_launch) {
+    auto launch = [&](auto kernel) {
+      kernel<<<(unsigned)(p.n_dkv + p.n_dq + p.n_sinks), AT_THREADS, 0, st>>>(q, k, v, d_o, a.lse, lse2, a.delta, (bf16_t*)a.dq, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len,
+                                                                             a.scale, a.rope_q, a.window, seqs, p.key_block0, p.key_blocks, slices, part, p.q_blocks,
+                                                                             p.dq_first, p.side_by_side, a.sinks, p.sink_blocks, a.sink_slices, sink_part);
+    };
+    if (p.halves) launch(attn_bwd_sinks_k<DH, true>);
+    else launch(attn_bwd_sinks_k<DH, false>);
+  } else {
+    auto launch_dq = [&](auto kernel) {
+      kernel<<<(unsigned)p.n_dq, AT_THREADS, 0, st>>>(q, k, v, d_o, a.lse, a.delta, (bf16_t*)a.dq, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.rope_q, a.window, seqs,
+                                                      p.q_blocks, a.sinks);
+    };
+    if (p.halves) launch_dq(attn_bwd_dq_sinks_k<DH, true>);
+    else launch_dq(attn_bwd_dq_sinks_k<DH, false>);
+    if (p.n_dkv > 0)
+      attn_bwd_dkv_window_k<DH><<<dim3((unsigned)p.key_blocks, a.Hkv * a.batch, part ? (unsigned)slices : 1u), KV_THREADS, 0, st>>>(
+          q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, p.key_block0, slices, part);
+    if (sink_part) launch_sinks((unsigned)a.sink_slices);
   }
+  bool own_done = false;
+  if (part || sink_part) {
+    const int first = p.key_block0 * KV_TILE;
+    const int64_t rows = part ? (int64_t)std::min(a.sinks, first) + n_total - first : a.sinks;
+    own_done = part && first <= a.q_start && a.dkc && !in_place;
+    attn_dkv_sum_sinks_k<DH><<<dim3((unsigned)cdiv(2 * rows * a.Hkv * (DH / 8), 256), a.batch), 256, 0, st>>>(
+        part, slices, first, sink_part, a.sink_slices, a.sinks, rows, a.Hkv, a.dk, a.dv, a.q_start, n_total, own_done ? (bf16_t*)a.dkc : nullptr, (bf16_t*)a.dvc, a.rope_k, seqs);
+  }
+  if (in_place) launch_sinks(1u);
+  if (a.dkc && !own_done) return own_rows_finish<DH>(a, st);
   return hipGetLastError();
 }
 
 hipError_t attn_forward_mfma(const AttnArgs& a, hipStream_t st) { return a.dh == 64 ? forward_dh<64>(a, st) : forward_dh<128>(a, st); }
-hipError_t attn_backward_mfma(const AttnArgs& a, hipStream_t st) { return a.dh == 64 ? backward_dh<64>(a, st) : backward_dh<128>(a, st); }
+hipError_t attn_backward_mfma(const AttnArgs& a, hipStream_t st) {
+  if (a.sinks > 0) return a.dh == 64 ? backward_sinks<64>(a, st) : backward_sinks<128>(a, st);
+  return a.dh == 64 ? backward_dh<64>(a, st) : backward_dh<128>(a, st);
+}
 
 }  // namespace sbp

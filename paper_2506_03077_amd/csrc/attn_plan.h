@@ -65,6 +65,9 @@ struct AttnBackwardPlan {
   int q_blocks;
   int64_t n_dkv, n_dq;                // workgroups
   bool one_launch, dq_first;          // dK/dV and dQ in one launch; those of dQ first
+  int sink_blocks;                    // with sinks: key blocks of a sequence that the queries past their windows walk (0: no such query),
+  bool sink_parts;                    // ... in slices whose sums meet in the scratch,
+  int64_t n_sinks;                    // ... and the workgroups of that, which one launch has too
   bool side_by_side;                  // one launch: the key blocks of a head side by side, else the heads of a key block
 };
 // most, most_prefix: workgroups up to which a call, one behind a prefix, is one launch where dK/dV comes first
@@ -78,6 +81,9 @@ inline AttnBackwardPlan attn_backward_plan(const AttnArgs& a, int most, int most
   p.parts = slices > 1 && a.dkv_scratch;
   p.in_turn = a.sinks == 0 && slices > 1 && !p.parts && blocks > 0 && blocks <= ATTN_IN_TURN_BLOCKS;
   p.n_dkv = blocks * (p.in_turn ? 2 : p.parts ? slices : 1);
+  p.sink_blocks = attn_sink_blocks(a);
+  p.sink_parts = p.sink_blocks > 0 && a.sink_slices > 1 && a.sink_scratch;
+  p.n_sinks = p.sink_parts ? (int64_t)p.sink_blocks * a.Hkv * a.batch * a.sink_slices : 0;
   p.q_blocks = (int)cdiv(a.q_len, tile);
   p.n_dq = (int64_t)p.q_blocks * a.Hq * a.batch;
   // The longer workgroups first, by their steps: last, they are a tail on a chip that is otherwise done.  A dQ tile sees at most its own keys and a window before them.
@@ -93,7 +99,7 @@ inline AttnBackwardPlan attn_backward_plan(const AttnArgs& a, int most, int most
   const int64_t dkv_steps = cdiv(seen_by, ATTN_KV_QUERIES) * (a.Hq / a.Hkv) / (p.parts ? slices : 1);
   p.dq_first = dq_steps > dkv_steps && p.n_dq <= ATTN_DQ_FIRST;
   const int64_t n = p.n_dkv + p.n_dq;
-  p.one_launch = a.sinks == 0 && p.n_dkv > 0 && (p.in_turn || (p.dq_first && a.q_start > 0) || n <= (a.q_start > 0 ? most_prefix : most));
+  p.one_launch = p.n_dkv > 0 && (p.in_turn || (p.dq_first && a.q_start > 0) || n <= (a.q_start > 0 ? most_prefix : most));
   // Workgroup b runs on XCD b % 8.  With the key blocks side by side an XCD has every eighth of them: where the chunk's own blocks, which ever fewer queries see, are
   // many, up to 2.4 times the work of another (2048 queries from 0, 28 / 4 heads 182 us, the heads of a block side by side 133, from 2048 344 / 328; 32 / 8 heads
   // 385 / 352 from 0, 790 / 769 from 6144).  Where they are an eighth or less, or each workgroup has a CU of its own, there is nothing to even out, and a head's

@@ -192,7 +192,9 @@ struct AttnArgs {
   // attn_dkv_scratch_bytes) that lets a workgroup take each
   int dkv_slices = 1;
   float* dkv_scratch = nullptr;
-  int sink_slices = 1;     // ... that the queries past a sink's window are cut into (attn_sink_slices); their sums meet in the same scratch
+  // ... that the queries past a sink's window are cut into (attn_sink_slices), and the scratch of theirs (attn_sink_scratch_bytes)
+  int sink_slices = 1;
+  float* sink_scratch = nullptr;
   // Optional rotary embedding of the chunk's queries folded into the attention kernels: cos/sin rows [c, dh/2] of the
   // chunk's positions.  Forward: q arrives un-rotated, is rotated on load and written back rotated (q must then be
   // writable); backward: q is the rotated tensor the forward left, and dq leaves the kernel already rotated back
