@@ -506,7 +506,8 @@ int32_t layer_backward_impl(const sbp_layer_cfg* c, const sbp_layer_weights* w, 
       aa.d_o = s.d_o; aa.dq = s.dq; aa.dk = s.dK; aa.dv = s.dV; aa.delta = s.delta;
       if (dt == DT_BF16) {
         aa.sink_slices = attn_sink_slices(aa, s.gemm_scratch_bytes / 4);
-        const size_t sums = align_up(attn_sink_scratch_bytes(aa, aa.sink_slices), 256);
+        size_t sums = align_up(attn_sink_scratch_bytes(aa, aa.sink_slices), 256);
+        if (sums > s.gemm_scratch_bytes / 4) sums = 0;
         if (sums) aa.sink_scratch = s.gemm_scratch;
         aa.dkv_slices = attn_dkv_slices(aa, s.gemm_scratch_bytes - sums);
         if (aa.dkv_slices > 1) aa.dkv_scratch = s.gemm_scratch + sums / sizeof(float);      // (idle between GEMMs)
@@ -1073,11 +1074,11 @@ int32_t streambp_attn_chunk_backward(const sbp_attn_cfg* c, const void* q, const
   if (workspace_bytes < attn_stats_bytes(c)) return fail(SBP_ERR_WORKSPACE, "workspace too small");
   AttnArgs a = attn_args(c);
   // with less than the query's bytes the same slices run one after the other: the same results
-  if ((a.dkv_slices > 1 || a.sink_slices > 1) && workspace_bytes >= streambp_attn_workspace_bytes(c)) {
+  if (workspace_bytes >= streambp_attn_workspace_bytes(c)) {
     char* scratch = (char*)workspace + attn_stats_bytes(c);
     const size_t parts = align_up(attn_dkv_scratch_bytes(a, a.dkv_slices), 256);
     if (a.dkv_slices > 1) a.dkv_scratch = (float*)scratch;
-    if (a.sink_slices > 1) a.sink_scratch = (float*)(scratch + parts);
+    if (attn_sink_blocks(a) > 0) a.sink_scratch = (float*)(scratch + parts);
   }
   a.q = q; a.k = k; a.v = v; a.o = (void*)o; a.lse = (float*)lse;
   a.d_o = d_o; a.dq = dq; a.dk = dk; a.dv = dv; a.delta = (float*)workspace;

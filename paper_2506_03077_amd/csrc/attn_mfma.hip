@@ -231,9 +231,8 @@ __device__ __forceinline__ void query_tile_of(int id, int n_qt, int heads, int& 
 
 // The key tiles of a workgroup's queries: those from kt0 on, the first that any of them sees in its window, up to n_tiles.  SINKS: before them those
 // of the first `sinks` keys from kv_first on, which every later query sees, as far as they lie before kt0.  A sink is one key more for the softmax and
-// for every product, so nothing else of the walk changes: tiles that a wave sees nothing of, which its workgroup walks between the sinks and the wave's own
-// window, are masked as a whole (a barrier paces the waves, so that skipping them would gain nothing).  The sinks may end in a tile from kt0 on, so every wave begins
-// with the first one.
+// for every product, so nothing else of the walk changes: a wave has two runs of tiles, those of the sinks (which may end in a tile from kt0 on) and those
+// of its own window, and skips what its workgroup walks between them.
 template <bool SINKS, int NK>
 struct KeyTiles {
   int kt0, n_window, sink0 = 0, n_sink = 0, kv_first, sink_end;      // keys kv_first .. sink_end - 1 are the sinks
@@ -247,6 +246,9 @@ struct KeyTiles {
   __device__ __forceinline__ int n() const { return n_sink + n_window; }
   __device__ __forceinline__ int at(int i) const { return SINKS && i < n_sink ? sink0 + i : kt0 - n_sink + i; }
   __device__ __forceinline__ int base() const { return kt0 - n_sink; }      // of the window's tiles: at(i) - i
+  __device__ __forceinline__ int sinks_to() const {                         // places before which all sinks lie
+    return sink_end <= kv_first ? 0 : n_sink + max(0, (sink_end - 1) / NK - kt0 + 1);
+  }
   // A row of tile t that some query may see in the place of one that none of the workgroup does (before the first key, between the sinks and `lo`, the first key of
   // the windows, behind the last key): what lies there is never read.
   __device__ __forceinline__ int safe_row(int t, int row, int lo, int rows_valid) const {
@@ -384,19 +386,32 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
   const uint32_t dst_k = __builtin_amdgcn_readfirstlane(lds_k + (uint32_t)(tid & ~63) * 16u), tile_bytes = (uint32_t)(TK * kv_stride * 2);
   // load p (of PIECES) of the pair V(i + V_AHEAD), K(i + K_AHEAD)
   constexpr int PIECES = 2 * LOADS;
-  auto issue_piece = [&](int p, int i) __attribute__((always_inline)) {
-    const bool is_k = p >= LOADS;
-    const int j = p % LOADS, ahead = is_k ? K_AHEAD : V_AHEAD, t = min(tile_of(i + ahead), t_max);
-    const char* src = (const char*)(is_k ? kbase : vbase) + (uint64_t)tile_bytes * (uint32_t)t;
-    const uint32_t to = dst_k + (uint32_t)(((is_k ? 0 : 4) + (i + ahead) % STAGES) * TILE64<DH> + j * LOADERS * 16);
+  struct Offsets { uint32_t of[SINKS ? PIECES : 1]; };      // SINKS: of the pieces' loads within their tiles
+  auto load_tile = [&](int p, int i) { return min(tile_of(i + (p >= LOADS ? K_AHEAD : V_AHEAD)), t_max); };
+  auto offsets = [&](int i) __attribute__((always_inline)) {
+    Offsets o;
     if constexpr (SINKS) {
-      if (t <= kt0) {
-        const int id = j * LOADERS + ((int)pin(threadIdx.x) & (LOADERS - 1)), row = id / (DH / 8), chunk = (id % (DH / 8)) ^ swz<DH>(row);      // (opaque: nothing of this is kept in a register)
-        dma16(src, (uint32_t)((tiles.safe_row(t, row, first_key(q_start + q0), n_total - t * TK) * kv_stride + chunk * 8) * 2), to);
-        return;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) o.of[p] = load_tile(p, i) == t_max ? voff_last[p % LOADS] : voff[p % LOADS];
+      if (load_tile(0, i) <= kt0) {      // among the first tiles of the walk only, and one branch for all pieces: a branch in front of each cost 3 us of 33 (777 queries, window 1024)
+        const int lo = first_key(q_start + q0), row = tid / (DH / 8);
+        const uint32_t chunk = (uint32_t)((tid % (DH / 8)) ^ swz<DH>(row)) * 16u, stride = (uint32_t)kv_stride * 2u;      // (the same for rows that lie 16 apart)
+        static_assert(LOADERS / (DH / 8) % 16 == 0, "rows of a load");
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+          const int t = load_tile(p, i);
+          if (t <= kt0) o.of[p] = (uint32_t)tiles.safe_row(t, row + p % LOADS * (LOADERS / (DH / 8)), lo, n_total - t * TK) * stride + chunk;
+        }
       }
     }
-    dma16(src, t == t_max ? voff_last[j] : voff[j], to);
+    return o;
+  };
+  auto issue_piece = [&](int p, int i, const Offsets& o) __attribute__((always_inline)) {
+    const bool is_k = p >= LOADS;
+    const int j = p % LOADS, ahead = is_k ? K_AHEAD : V_AHEAD, t = load_tile(p, i);
+    const char* src = (const char*)(is_k ? kbase : vbase) + (uint64_t)tile_bytes * (uint32_t)t;
+    dma16(src, SINKS ? o.of[p % (SINKS ? PIECES : 1)] : t == t_max ? voff_last[j] : voff[j],
+          dst_k + (uint32_t)(((is_k ? 0 : 4) + (i + ahead) % STAGES) * TILE64<DH> + j * LOADERS * 16));
   };
 
   bf16x8 ones;
@@ -421,15 +436,17 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
   const float sl = scale * LOG2E;
   // steps in which some (query, key) pair of the wave is visible: tiles wave_lo_min / TK .. wave_last_key / TK
   const int step_t = SPLIT ? 2 : 1, first_t = tiles.base() + (SPLIT ? grp : 0);
-  const int act0 = SINKS ? 0 : max(0, (wave_lo_min / TK - first_t + step_t - 1) / step_t);
+  const int act0 = max(0, (wave_lo_min / TK - first_t + step_t - 1) / step_t);
   const int act1 = qw0 < c && wave_last_key >= 0 ? min(n_it, (wave_last_key / TK - first_t + step_t) / step_t) : 0;
+  const int sinks1 = SINKS ? max(0, min(act1, SPLIT ? (tiles.sinks_to() - grp + 1) / 2 : tiles.sinks_to())) : 0;      // SINKS: and before them 0 .. sinks1 - 1
 
   // LDS addresses of fragments, one step after the other: of K rows of the present tile, of V transposed of the previous one
+  const int first_run = SINKS ? 0 : act0;      // where the wave's first run begins
   uint32_t fr[KS], ft[DB];
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk) fr[kk] = pin(lds_k + frag16_rows<DH>(kk) + (uint32_t)(act0 % STAGES) * TILE64<DH>);
+  for (int kk = 0; kk < KS; ++kk) fr[kk] = pin(lds_k + frag16_rows<DH>(kk) + (uint32_t)(first_run % STAGES) * TILE64<DH>);
 #pragma unroll
-  for (int d = 0; d < DB; ++d) ft[d] = pin(lds_v + frag16_tr<DH>(d) + (uint32_t)(act0 % STAGES) * TILE64<DH>);
+  for (int d = 0; d < DB; ++d) ft[d] = pin(lds_v + frag16_tr<DH>(d) + (uint32_t)(first_run % STAGES) * TILE64<DH>);
   auto to_next = [&](int i) { return i % STAGES == STAGES - 1 ? (uint32_t)-(int)((STAGES - 1) * TILE64<DH>) : (uint32_t)TILE64<DH>; };      // from the stage of tile i
 
   // fragment reads run RING - 1 fragments (two MFMAs each) ahead of the products
@@ -486,13 +503,16 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int qpos = q_start + min(qw0 + b * 16 + li, c - 1);
-        const Seen<SINKS> seen(qpos, first_key(qpos), kv_first, tiles.sink_end, k0 + 4 * lg);
+        auto mask = [&](const auto& seen) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
+          for (int kb = 0; kb < 4; ++kb) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) s[b][kb][r] = seen(kb * 16 + r) ? s[b][kb][r] : -INFINITY;
-          __builtin_amdgcn_sched_barrier(0);
-        }
+            for (int r = 0; r < 4; ++r) s[b][kb][r] = seen(kb * 16 + r) ? s[b][kb][r] : -INFINITY;
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        };
+        if (SINKS && k0 < tiles.sink_end) mask(Seen<SINKS>(qpos, first_key(qpos), kv_first, tiles.sink_end, k0 + 4 * lg));
+        else mask(Seen<false>(qpos, first_key(qpos), kv_first, tiles.sink_end, k0 + 4 * lg));
       }
     }
 #pragma unroll
@@ -514,6 +534,7 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
 #pragma unroll
       for (int b = 0; b < 2; ++b) mx[b] = max_raw(mx[b], sM[grp ^ 1][wave & 3][b * 16 + li]);
     }
+    const Offsets o = offsets(i);
     // The maximum (and with it the rescale of O) only moves when some query of the wave sees a new one.
     if (__builtin_amdgcn_ballot_w64(mx[0] > m_raw[0] || mx[1] > m_raw[1]) != 0) {
 #pragma unroll
@@ -541,7 +562,7 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
     for (int x = 0; x < 4; ++x) {        // eight probabilities at a time, the loads spread between them
       const int b = x >> 1, kk = x & 1;
 #pragma unroll
-      for (int p = x * PIECES / 4; p < (x + 1) * PIECES / 4; ++p) issue_piece(p, i);
+      for (int p = x * PIECES / 4; p < (x + 1) * PIECES / 4; ++p) issue_piece(p, i, o);
       __builtin_amdgcn_sched_barrier(0);
       float pe[8];
 #pragma unroll
@@ -558,9 +579,11 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
   if (n_it > 0) {
     // loads are issued in the order K(0) | V(0) K(1) | V(1) K(2) ...: per softmax slot i, V(i + V_AHEAD) and K(i + K_AHEAD)
 #pragma unroll
-    for (int j = 0; j <= V_AHEAD; ++j)
+    for (int j = 0; j <= V_AHEAD; ++j) {
+      const Offsets o = offsets(j - 1 - V_AHEAD);
 #pragma unroll
-      for (int p = j == 0 ? LOADS : 0; p < PIECES; ++p) issue_piece(p, j - 1 - V_AHEAD);
+      for (int p = j == 0 ? LOADS : 0; p < PIECES; ++p) issue_piece(p, j - 1 - V_AHEAD, o);
+    }
     AT_WAIT_VM(PIECES * V_AHEAD);
     AT_SLOT_BARRIER();
     if (grp == 1) AT_SLOT_BARRIER();        // group 1 falls one slot behind ...
@@ -579,26 +602,41 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
     };
     auto skip = [&]() __attribute__((always_inline)) {      // a tile that no query of the wave sees
       into_softmax();
+      const Offsets o = offsets(i);
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) issue_piece(p, i);
+      for (int p = 0; p < PIECES; ++p) issue_piece(p, i, o);
       into_multiply();
     };
-    while (i < min(act0, n_it)) skip();
-    if (i < act1) {      // the wave's tiles: one run of steps, without a branch around the products
-      __builtin_amdgcn_s_setprio(1);
-      do {
-        float mx[2];
-        qk(i);
-        __builtin_amdgcn_s_setprio(0);
-        row_max(i, mx);
-        into_softmax();
-        softmax(i, mx);
-        into_multiply();
+    auto steps = [&](int from, int to) __attribute__((always_inline)) {
+      while (i < min(from, n_it)) skip();
+      if (i < to) {      // the wave's tiles: one run of steps, without a branch around the products
         __builtin_amdgcn_s_setprio(1);
-        pv(i - 1);
-      } while (i < act1);
-      __builtin_amdgcn_s_setprio(0);
-    }
+        do {
+          float mx[2];
+          qk(i);
+          __builtin_amdgcn_s_setprio(0);
+          row_max(i, mx);
+          into_softmax();
+          softmax(i, mx);
+          into_multiply();
+          __builtin_amdgcn_s_setprio(1);
+          pv(i - 1);
+        } while (i < to);
+        __builtin_amdgcn_s_setprio(0);
+      }
+    };
+    if constexpr (SINKS) {
+#pragma unroll 1
+      for (int run = 0; run < 2; ++run) {
+        const int from = run ? max(act0, sinks1) : 0;      // the addresses stand at the stage of tile sinks1 after the first run
+        const uint32_t move = run ? (uint32_t)(from % STAGES - sinks1 % STAGES) * TILE64<DH> : 0u;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) fr[kk] = pin(fr[kk] + move);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) ft[d] = pin(ft[d] + move);
+        steps(from, run ? act1 : sinks1);
+      }
+    } else steps(act0, act1);
     while (i < n_it) skip();
     AT_WAIT_VM(0);
     if (grp == 0) AT_SLOT_BARRIER();        // ... and group 0 waits for it here: both execute the same number of barriers
@@ -812,15 +850,17 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
   };
   // steps in which some (query, key) pair of the wave is visible
   const int step_t = SPLIT ? 2 : 1, first_t = tiles.base() + (SPLIT ? grp : 0);
-  const int act0 = SINKS ? 0 : max(0, (wave_lo_min / NK - first_t + step_t - 1) / step_t);
+  const int act0 = max(0, (wave_lo_min / NK - first_t + step_t - 1) / step_t);
   const int act1 = qw0 < c && wave_last_key >= 0 ? min(n_it, (wave_last_key / NK - first_t + step_t) / step_t) : 0;
+  const int sinks1 = SINKS ? max(0, min(act1, SPLIT ? (tiles.sinks_to() - grp + 1) / 2 : tiles.sinks_to())) : 0;      // as in the forward kernel
 
   // LDS addresses of fragments, one step after the other: of K (and V) rows of the present tile, of K transposed of the previous one
+  const int first_run = SINKS ? 0 : act0;      // where the wave's first run begins
   uint32_t fr[KS], ft[DB];
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk) fr[kk] = pin(lds_k + frag16_rows<DH>(kk) + (uint32_t)(act0 % STAGES) * STAGE);
+  for (int kk = 0; kk < KS; ++kk) fr[kk] = pin(lds_k + frag16_rows<DH>(kk) + (uint32_t)(first_run % STAGES) * STAGE);
 #pragma unroll
-  for (int d = 0; d < DB; ++d) ft[d] = pin(lds_k + frag16_tr<DH>(d) + (uint32_t)((act0 + (MOVE_LATE ? STAGES - 1 : 0)) % STAGES) * STAGE);
+  for (int d = 0; d < DB; ++d) ft[d] = pin(lds_k + frag16_tr<DH>(d) + (uint32_t)((first_run + (MOVE_LATE ? STAGES - 1 : 0)) % STAGES) * STAGE);
   auto to_next = [&](int i) { return i % STAGES == STAGES - 1 ? (uint32_t)-(int)((STAGES - 1) * STAGE) : STAGE; };      // from the stage of tile i
   auto move_rows = [&](int i) __attribute__((always_inline)) {
     const uint32_t move = to_next(i);
@@ -876,13 +916,15 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int qpos = q_start + min(qw0 + b * 16 + (l & 15), c - 1);
-        const Seen<SINKS> seen(qpos, first_key(qpos), kv_first, tiles.sink_end, k0 + 4 * (l >> 4));
+        auto mask = [&](const auto& seen) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
+          for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x.s[b][kb][r] = seen(kb * 16 + r) ? x.s[b][kb][r] : -INFINITY;     // exp2(-inf) = 0
-          __builtin_amdgcn_sched_barrier(0);
-        }
+            for (int r = 0; r < 4; ++r) x.s[b][kb][r] = seen(kb * 16 + r) ? x.s[b][kb][r] : -INFINITY;     // exp2(-inf) = 0
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        };
+        mask(Seen<SINKS>(qpos, first_key(qpos), kv_first, tiles.sink_end, k0 + 4 * (l >> 4)));
       }
     }
 #pragma unroll
@@ -943,22 +985,37 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
       ++i;
     };
     auto skip = [&]() __attribute__((always_inline)) { into_vector(); into_multiply(); };      // a tile that no query of the wave sees
-    while (i < min(act0, n_it)) skip();
-    if (i < act1) {
-      __builtin_amdgcn_s_setprio(1);
-      do {
-        Scores x;
-        Operand ds;
-        first(x, i);
-        into_vector();
-        if (MOVE_LATE) { move_rows(i); move_tr(i + STAGES - 1); }
-        vector(x, ds, i);
-        into_multiply();
+    auto steps = [&](int from, int to) __attribute__((always_inline)) {
+      while (i < min(from, n_it)) skip();
+      if (i < to) {
         __builtin_amdgcn_s_setprio(1);
-        second(ds, i - 1);
-      } while (i < act1);
-      __builtin_amdgcn_s_setprio(0);
-    }
+        do {
+          Scores x;
+          Operand ds;
+          first(x, i);
+          into_vector();
+          if (MOVE_LATE) { move_rows(i); move_tr(i + STAGES - 1); }
+          vector(x, ds, i);
+          into_multiply();
+          __builtin_amdgcn_s_setprio(1);
+          second(ds, i - 1);
+        } while (i < to);
+        __builtin_amdgcn_s_setprio(0);
+      }
+    };
+    if constexpr (SINKS) {
+#pragma unroll 1
+      for (int run = 0; run < 2; ++run) {
+        const int from = run ? max(act0, sinks1) : 0;
+        auto move = [&](int late) { return run ? (uint32_t)((from + late) % STAGES - (sinks1 + late) % STAGES) * STAGE : 0u; };
+        const uint32_t move_fr = move(0), move_ft = move(MOVE_LATE ? STAGES - 1 : 0);
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) fr[kk] = pin(fr[kk] + move_fr);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) ft[d] = pin(ft[d] + move_ft);
+        steps(from, run ? act1 : sinks1);
+      }
+    } else steps(act0, act1);
     while (i < n_it) skip();
     AT_WAIT_VM(0);
     if (grp == 0) AT_SLOT_BARRIER();        // both groups execute the same number of barriers
@@ -1061,13 +1118,14 @@ __global__ __launch_bounds__(AT_THREADS) void attn_bwd_dq_sinks_k(const bf16_t* 
 // apart | with room, 28 / 4 heads: 512 queries from 0 228 / 123 | 143 | 41 us, 2048 from 0 401 / 357 | 459 | 177; 512 from 2560 (96 blocks) 135 /
 // 124 | 184 | 123, from 2816 (104 blocks, whose 208 workgroups leave dQ too few CUs) 136 / 152 | 188 | 127, from 3500 145 / 198 | 205 | 146.
 //
-// With sinks the queries of a key fall into two: those of its window, the window kernel's as without sinks, and, for the sinks themselves, the
-// later ones.  SINKS_KEYS: the latter, `key_block` from the block of kv_first on; their sums are left for, or added to, the sinks' rows alone.  WINDOW_KEYS: the former; in
-// the place of keys before the first window another row is read, so that what was evicted between the sinks and the window may hold anything.
-// Both hand P over as fp16 where ALL_KEYS has bf16 (heads of 128), 2^15 P, the largest of which fp16 holds, so that the smallest that counts does not leave its normal range;
+// With sinks the queries of a key fall into two: those of its window, and, for the sinks themselves, the later ones.  SINKS: a workgroup walks either for its keys; `sink`:
+// the latter, `key_block` from the block of kv_first on, and their sums are left for, or added to, the sinks' rows alone.  One code with the limits in registers:
+// with a copy for each, the kernel that has dQ too ran out of them, and two that spilled in dQ's loop, whose counted waits then wait for everything, cost 22 % (2048 queries
+// behind 30720, window 4096, 28 / 4 heads, backward 378 without sinks, 462 us).  In the place of keys that none of its queries sees another row is read, so that what
+// was evicted between the sinks and the window may hold anything.
+// P goes to its partner as fp16 where it is bf16 without sinks (heads of 128), 2^15 P, the largest of which fp16 holds, so that the smallest that counts does not leave its normal range;
 // the exponent, a power of two, costs nothing and leaves with the last factor.  dS is then rounded to bf16 once instead of twice: error of dk against fp64 2.4e-3
 // instead of 2.9e-3, of which its own rounding to bf16 is 1.7e-3.
-enum DkvPart { ALL_KEYS, WINDOW_KEYS, SINKS_KEYS };
 constexpr float P16_LOG2 = 15.f;
 template <int DH> constexpr bool P16_HEADS = !FP32_STATS<DH>;
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -1083,25 +1141,34 @@ struct DkvShared {
   float sL[KV_STAGES][QT];                        // (log2-domain) log-sum-exp of the tile's queries
   float sDl[KV_STAGES][QT];                       // delta of the tile's queries
 };
-template <int DH, bool IN_TURN, DkvPart PART = ALL_KEYS>
+template <int DH, bool IN_TURN, bool SINKS = false>
 __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int bh, int slice, const bf16_t* __restrict__ q,
                                           const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o,
                                           const float* __restrict__ lse2, const float* __restrict__ delta, float* __restrict__ dk,
                                           float* __restrict__ dv, int Hq, int Hkv, int q_start, int c, float scale, int window, const AttnSeqs& seqs,
-                                          int key_block0, int slices, float* __restrict__ part, int sinks = 0) {
-  constexpr bool SINK = PART == SINKS_KEYS, P16 = PART != ALL_KEYS && P16_HEADS<DH>;
-  static_assert(!(IN_TURN && PART != ALL_KEYS), "with sinks, shares are taken with a break");
+                                          int key_block0, int slices, float* __restrict__ part, bool sink = false, int sinks = 0) {
+  constexpr bool P16 = SINKS && P16_HEADS<DH>;
+  static_assert(!(IN_TURN && SINKS), "with sinks, shares are taken with a break");
   const int sq = bh / Hkv, kvh = bh - sq * Hkv, kv_first = seqs.first[sq];
-  const int sink_end = kv_first + min(sinks, max(0, q_start + c - kv_first));
-  if (SINK) key_block0 = kv_first / KV_TILE;
-  // rows of the parts: first_part .. last_part - 1
-  const int first_part = SINK ? kv_first : key_block0 * KV_TILE, last_part = SINK ? sink_end : q_start + c;
-  const int64_t part_rows = SINK ? sinks : q_start + c - first_part;
+  // SINKS: keys that count, kv_first .. key_end - 1, each for the queries from `past` to `reach` - 1 behind it; rows of K and V that are read, and of dK and dV that are written, from
+  // read_lo resp. write_lo on
+  int key_end = q_start + c, past = 0, reach = 0, read_lo = 0, write_lo = 0;
+  if constexpr (SINKS) {
+    reach = min(window, key_end);
+    read_lo = max(kv_first, q_start - reach + 1);
+    if (sink) {
+      past = reach;
+      reach = key_end;
+      key_end = kv_first + min(sinks, max(0, key_end - kv_first));
+      read_lo = write_lo = kv_first;
+      key_block0 = kv_first / KV_TILE;
+    }
+  }
   {
     const int64_t nq = (int64_t)sq * c * Hq, nk = (int64_t)sq * c * Hkv * DH;
     q += nq * DH; d_o += nq * DH; lse2 += 2 * nq; delta += 2 * nq;
     k += nk; v += nk; dk += nk; dv += nk;
-    if (part) part += (int64_t)sq * slices * 2 * part_rows * Hkv * DH;
+    if (part) part += (int64_t)sq * slices * 2 * (SINKS && sink ? sinks : q_start + c - key_block0 * KV_TILE) * Hkv * DH;
   }
   auto& sQD = sh.sQD;
   auto& sP = sh.sP;
@@ -1117,12 +1184,7 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
   const int kw0 = key0 + kb * 32;      // a lane has the keys li and 16 + li from there on
   auto key_of = [&](int b) { return kw0 + b * 16 + li; };
   auto key_row = [&](int b) { return (int64_t)min(key_of(b), n_total - 1); };
-  auto read_row = [&](int b) {      // of K and V
-    int key = key_of(b);
-    if (SINK) key = max(min(key, sink_end - 1), kv_first);      // (a sink's, for keys that are none)
-    if (PART == WINDOW_KEYS) key = max(max(key, kv_first), q_start - min(window, n_total) + 1);
-    return (int64_t)min(key, n_total - 1);
-  };
+  auto read_row = [&](int b) { return SINKS ? (int64_t)min(max(min(key_of(b), key_end - 1), read_lo), n_total - 1) : key_row(b); };      // of K and V
   const int64_t kv_stride = (int64_t)Hkv * DH;
   const int64_t q_stride = (int64_t)Hq * DH;
 
@@ -1164,12 +1226,11 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
 
   // query tiles that can see at least one key of this workgroup: query position >= key0
   // ... and, under a sliding window, query position <= last key of the workgroup + window - 1
-  // SINK: those of which some query has passed its window
-  const int past = SINK ? min(window, n_total) : 0;
-  const int qt_first = max(0, max(key0, SINK ? kv_first : 0) - q_start + past) / QT;
+  const int qt_first = SINKS ? max(0, max(key0, kv_first) - q_start + past) / QT : max(0, key0 - q_start) / QT;
   int n_qt = (c + QT - 1) / QT;
-  if (!SINK && window > 0) n_qt = min(n_qt, max(0, key0 + KV_TILE - 1 + window - 1 - q_start) / QT + 1);
-  const int n_all = key0 + KV_TILE <= kv_first || (SINK && key0 >= sink_end) ? 0 : max(0, n_qt - qt_first) * G;      // (a sequence of several may hide blocks that others see)
+  if (SINKS) n_qt = min(n_qt, max(0, key0 + KV_TILE - 2 + (reach - q_start)) / QT + 1);
+  else if (window > 0) n_qt = min(n_qt, max(0, key0 + KV_TILE - 1 + window - 1 - q_start) / QT + 1);
+  const int n_all = key0 + KV_TILE <= kv_first || (SINKS && key0 >= key_end) ? 0 : max(0, n_qt - qt_first) * G;      // (a sequence of several may hide blocks that others see)
   auto share = [&](int z) { return (int)((int64_t)n_all * z / slices); };      // first step of share z
   for (int z = part ? slice : 0, z_last = IN_TURN ? 0 : part ? slice : slices - 1; z <= z_last; ++z) {
   const int it0 = IN_TURN ? 0 : share(z), n_iter = (IN_TURN ? n_all : share(z + 1)) - it0;
@@ -1192,7 +1253,8 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
   // One 64-query tile = two 32-query blocks.  `active`: the wave has a valid key and some query of the tile is
   // at or after its first key (the same answer for both waves of a key block).
   auto tile_active = [&](int qbase) {
-    if (SINK) return kw0 < sink_end && kw0 + 31 >= kv_first && q_start + min(qbase + QT, c) - 1 >= max(kw0, kv_first) + past;
+    if (SINKS)
+      return kw0 < key_end && kw0 + 31 >= kv_first && q_start + min(qbase + QT, c) - 1 >= max(kw0, kv_first) + past && q_start + qbase - reach < kw0 + 31;
     return kw0 < n_total && q_start + min(qbase + QT, c) - 1 >= kw0 && kw0 + 31 >= kv_first &&
            (window == 0 || q_start + qbase - window < kw0 + 31);     // the tile's first query still reaches the wave's last key
   };
@@ -1276,14 +1338,16 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
     auto vector = [&]() __attribute__((always_inline)) {
       const uint32_t stat = stat_lane + (uint32_t)(j % KV_STAGES) * QT * 4;
       if constexpr (RP) {
-        const bool diag = SINK || (q_start + qbase < kw0 + 31) || (qbase + QT > c) || kw0 < kv_first ||   // some pair masked, or ragged query tile
-                          (window > 0 && q_start + qbase + QT - 1 - window >= kw0);
+        const bool diag = SINKS ? (q_start + qbase < kw0 + 31 + past) || (qbase + QT > c) || kw0 < kv_first || kw0 + 31 >= key_end || q_start + qbase + QT - 1 - reach >= kw0
+                                : (q_start + qbase < kw0 + 31) || (qbase + QT > c) || kw0 < kv_first ||   // some pair masked, or ragged query tile
+                                      (window > 0 && q_start + qbase + QT - 1 - window >= kw0);
         if (diag) {
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             // query 4 lg + e of the tile sees the key for from <= e < from + n: one unsigned comparison
-            const int key = key_of(b), lo = max(0, key - q_start + past), hi = !SINK && window > 0 ? min(c, key + min(window, n_total) - q_start) : c;
-            const uint32_t n = key < kv_first || (SINK && key >= sink_end) ? 0u : (uint32_t)max(0, hi - lo);
+            const int key = key_of(b), lo = max(0, key - q_start + past);
+            const int hi = SINKS ? min(c, key + (reach - q_start)) : window > 0 ? min(c, key + min(window, n_total) - q_start) : c;
+            const uint32_t n = key < kv_first || (SINKS && key >= key_end) ? 0u : (uint32_t)max(0, hi - lo);
             const int from = lo - qbase - 4 * lg;
 #pragma unroll
             for (int qb = 0; qb < 4; ++qb) {
@@ -1412,14 +1476,14 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
     if constexpr (IN_TURN) close();
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      if (key_of(b) >= last_part || (SINK && key_of(b) < kv_first)) continue;
+      if (key_of(b) >= key_end || (SINKS && key_of(b) < write_lo)) continue;
       if constexpr (IN_TURN) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) *(f32x4*)(out_of(b) + d * 16) = sum[b][d];
       } else {
         // several workgroups per key block: each leaves its sum in its own slice [workgroup][dk | dv][key][kv head][DH]
-        const int64_t first = first_part;
-        float* to = part ? part + ((int64_t)z * 2 + (RP ? 1 : 0)) * part_rows * kv_stride + (key_of(b) - first) * kv_stride + (int64_t)kvh * DH + 4 * lg : out_of(b);
+        const int64_t first = SINKS && sink ? kv_first : (int64_t)key_block0 * KV_TILE, rows = SINKS && sink ? sinks : n_total - first;
+        float* to = part ? part + ((int64_t)z * 2 + (RP ? 1 : 0)) * rows * kv_stride + (key_of(b) - first) * kv_stride + (int64_t)kvh * DH + 4 * lg : out_of(b);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
           f32x4 u = part ? f32x4{0.f, 0.f, 0.f, 0.f} : *(f32x4*)(to + d * 16);
@@ -1451,29 +1515,22 @@ __global__ __launch_bounds__(KV_THREADS) void attn_bwd_dkv_mfma_k(const bf16_t* 
                        seqs, key_block0, slices, part);
 }
 
-template <int DH>
-__global__ __launch_bounds__(KV_THREADS) void attn_bwd_dkv_window_k(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
-                                                                  const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o,
-                                                                  const float* __restrict__ lse2, const float* __restrict__ delta,
-                                                                  float* __restrict__ dk, float* __restrict__ dv, int Hq, int Hkv,
-                                                                  int q_start, int c, float scale, int window, const AttnSeqs seqs,
-                                                                  int key_block0, int slices, float* __restrict__ part) {
-  __shared__ __attribute__((aligned(1024))) DkvShared<DH> sh;
-  dkv_block<DH, false, WINDOW_KEYS>(sh, blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window,
-                       seqs, key_block0, slices, part);
-}
-// dK/dV of the sinks from the queries that have passed their window: blockIdx.x: 128-key block from that of kv_first on
+// With sinks: n_window workgroups of the windows, then those of the sinks
 template <int DH>
 __global__ __launch_bounds__(KV_THREADS) void attn_bwd_dkv_sinks_k(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
                                                                    const bf16_t* __restrict__ v, const bf16_t* __restrict__ d_o,
                                                                    const float* __restrict__ lse2, const float* __restrict__ delta,
                                                                    float* __restrict__ dk, float* __restrict__ dv, int Hq, int Hkv,
                                                                    int q_start, int c, float scale, int window, const AttnSeqs seqs,
-                                                                   int slices, float* __restrict__ part, int sinks) {
+                                                                   int key_block0, int key_blocks, int slices, float* __restrict__ part, int n_window,
+                                                                   int sinks, int sink_blocks, int sink_slices, float* __restrict__ sink_part) {
   __shared__ __attribute__((aligned(1024))) DkvShared<DH> sh;
-  dkv_block<DH, false, SINKS_KEYS>(sh, blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window,
-                             seqs, 0, slices, part, sinks);
+  const bool sink = (int)blockIdx.x >= n_window;
+  const int b = (int)blockIdx.x - (sink ? n_window : 0), of = sink ? sink_blocks : key_blocks, r = b / of, kv_heads = Hkv * seqs.n;
+  dkv_block<DH, false, true>(sh, b - r * of, r % kv_heads, r / kv_heads, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window, seqs, key_block0,
+                             sink ? sink_slices : slices, sink ? sink_part : part, sink, sinks);
 }
+
 // dK/dV and dQ in one launch, the longer workgroups first: for chunks that are a few rounds of the chip, where each
 // launch on its own leaves CUs idle at its end (AttnBackwardPlan).
 template <int DH, bool SPLIT, bool IN_TURN>
@@ -1512,19 +1569,15 @@ __global__ __launch_bounds__(AT_THREADS) void attn_bwd_sinks_k(BWD_PARAMS, int s
   __shared__ __attribute__((aligned(1024))) union { DkvShared<DH> dkv; DqShared<DH, SPLIT> dq; } sh;
   const int kv_heads = Hkv * seqs.n, heads = Hq * seqs.n, n_dkv = key_blocks * kv_heads * (part ? slices : 1), n_dq = q_blocks * heads;
   int b = (int)blockIdx.x;
-  if (b >= n_dkv + n_dq) {
-    b -= n_dkv + n_dq;
-    const int block = b % sink_blocks, r = b / sink_blocks;
-    dkv_block<DH, false, SINKS_KEYS>(sh.dkv, block, r % kv_heads, r / kv_heads, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window, seqs, 0,
-                                     sink_slices, sink_part, sinks);
-    return;
-  }
-  if (dq_first) b = b < n_dq ? b + n_dkv : b - n_dq;
-  if (b < n_dkv) {
-    const int of = side_by_side ? key_blocks : n_dkv / key_blocks, slow = __builtin_amdgcn_readfirstlane(b / of), fast = b - slow * of;
-    const int r = side_by_side ? slow : fast;
-    dkv_block<DH, false, WINDOW_KEYS>(sh.dkv, side_by_side ? fast : slow, r % kv_heads, r / kv_heads, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale,
-                                      window, seqs, key_block0, slices, part);
+  const bool sink = b >= n_dkv + n_dq;
+  if (sink) b -= n_dkv + n_dq;
+  else if (dq_first) b = b < n_dq ? b + n_dkv : b - n_dq;
+  if (sink || b < n_dkv) {
+    const int of = sink ? sink_blocks : side_by_side ? key_blocks : n_dkv / key_blocks, slow = __builtin_amdgcn_readfirstlane(b / of), fast = b - slow * of;
+    const bool by_head = sink || side_by_side;
+    const int r = by_head ? slow : fast;
+    dkv_block<DH, false, true>(sh.dkv, by_head ? fast : slow, r % kv_heads, r / kv_heads, q, k, v, d_o, lse2, delta, dk, dv, Hq, Hkv, q_start, c, scale, window, seqs,
+                               key_block0, sink ? sink_slices : slices, sink ? sink_part : part, sink, sinks);
   } else {
     const int i = b - n_dkv;
     int qt = q_blocks - 1 - i / heads, bh = i % heads;
@@ -1629,7 +1682,7 @@ __global__ __launch_bounds__(256) void attn_dkv_sum_sinks_k(const float* __restr
 // delta[h, t] = sum_j d_o[t,h,j] * o[t,h,j]  (DH / 8 lanes per (t, h), 16 bytes of each tensor per lane)
 // also lse2[h, t] = lse[h, t] * log2(e), the form the dK/dV kernel's exp2 wants (one multiply per (t, h) here
 // instead of one per score there); 64-wide heads, whose exponents are natural differences: lse[h, t] itself
-// P16: less P16_LOG2 (see DkvPart)
+// P16: less P16_LOG2 (see DkvShared)
 template <int DH, bool P16>
 __device__ __forceinline__ void delta_block(const bf16_t* __restrict__ o, const bf16_t* __restrict__ d_o, const float* __restrict__ lse,
                                             float* __restrict__ delta, int Hq, int c) {
@@ -1768,9 +1821,11 @@ static hipError_t backward_sinks(const AttnArgs& a, hipStream_t st) {
   const int slices = std::max(1, a.dkv_slices), n_total = a.q_start + a.q_len;
   float *part = p.parts ? a.dkv_scratch : nullptr, *sink_part = p.sink_parts ? a.sink_scratch : nullptr;
   const bf16_t *q = (const bf16_t*)a.q, *k = (const bf16_t*)a.k, *v = (const bf16_t*)a.v, *d_o = (const bf16_t*)a.d_o;
-  auto launch_sinks = [&](unsigned workgroups) {      // of a key block
-    attn_bwd_dkv_sinks_k<DH><<<dim3((unsigned)p.sink_blocks, a.Hkv * a.batch, workgroups), KV_THREADS, 0, st>>>(
-        q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, a.sink_slices, sink_part, a.sinks);
+  auto launch_dkv = [&](int64_t n_window, int64_t n_sinks) {
+    if (n_window + n_sinks > 0)
+      attn_bwd_dkv_sinks_k<DH><<<(unsigned)(n_window + n_sinks), KV_THREADS, 0, st>>>(q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs,
+                                                                                     p.key_block0, p.key_blocks, slices, part, (int)n_window, a.sinks, p.sink_blocks, a.sink_slices,
+                                                                                     sink_part);
   };
   const bool in_place = p.sink_blocks > 0 && !sink_part;      // the sinks' shares one after the other, added where they belong once the windows' are
   if (p.one_launch) {
@@ -1788,10 +1843,7 @@ static hipError_t backward_sinks(const AttnArgs& a, hipStream_t st) {
     };
     if (p.halves) launch_dq(attn_bwd_dq_sinks_k<DH, true>);
     else launch_dq(attn_bwd_dq_sinks_k<DH, false>);
-    if (p.n_dkv > 0)
-      attn_bwd_dkv_window_k<DH><<<dim3((unsigned)p.key_blocks, a.Hkv * a.batch, part ? (unsigned)slices : 1u), KV_THREADS, 0, st>>>(
-          q, k, v, d_o, lse2, a.delta, a.dk, a.dv, a.Hq, a.Hkv, a.q_start, a.q_len, a.scale, a.window, seqs, p.key_block0, slices, part);
-    if (sink_part) launch_sinks((unsigned)a.sink_slices);
+    launch_dkv(p.n_dkv, p.n_sinks);
   }
   bool own_done = false;
   if (part || sink_part) {
@@ -1801,7 +1853,7 @@ static hipError_t backward_sinks(const AttnArgs& a, hipStream_t st) {
     attn_dkv_sum_sinks_k<DH><<<dim3((unsigned)cdiv(2 * rows * a.Hkv * (DH / 8), 256), a.batch), 256, 0, st>>>(
         part, slices, first, sink_part, a.sink_slices, a.sinks, rows, a.Hkv, a.dk, a.dv, a.q_start, n_total, own_done ? (bf16_t*)a.dkc : nullptr, (bf16_t*)a.dvc, a.rope_k, seqs);
   }
-  if (in_place) launch_sinks(1u);
+  if (in_place) launch_dkv(0, (int64_t)p.sink_blocks * a.Hkv * a.batch);
   if (a.dkc && !own_done) return own_rows_finish<DH>(a, st);
   return hipGetLastError();
 }

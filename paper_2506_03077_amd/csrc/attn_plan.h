@@ -66,7 +66,7 @@ struct AttnBackwardPlan {
   int64_t n_dkv, n_dq;                // workgroups
   bool one_launch, dq_first;          // dK/dV and dQ in one launch; those of dQ first
   int sink_blocks;                    // with sinks: key blocks of a sequence that the queries past their windows walk (0: no such query),
-  bool sink_parts;                    // ... in slices whose sums meet in the scratch,
+  bool sink_parts;                    // ... in slices whose sums meet in the scratch (without it a launch of its own, that walks them in turn),
   int64_t n_sinks;                    // ... and the workgroups of that, which one launch has too
   bool side_by_side;                  // one launch: the key blocks of a head side by side, else the heads of a key block
 };
@@ -82,7 +82,7 @@ inline AttnBackwardPlan attn_backward_plan(const AttnArgs& a, int most, int most
   p.in_turn = a.sinks == 0 && slices > 1 && !p.parts && blocks > 0 && blocks <= ATTN_IN_TURN_BLOCKS;
   p.n_dkv = blocks * (p.in_turn ? 2 : p.parts ? slices : 1);
   p.sink_blocks = attn_sink_blocks(a);
-  p.sink_parts = p.sink_blocks > 0 && a.sink_slices > 1 && a.sink_scratch;
+  p.sink_parts = p.sink_blocks > 0 && a.sink_scratch;
   p.n_sinks = p.sink_parts ? (int64_t)p.sink_blocks * a.Hkv * a.batch * a.sink_slices : 0;
   p.q_blocks = (int)cdiv(a.q_len, tile);
   p.n_dq = (int64_t)p.q_blocks * a.Hq * a.batch;

@@ -245,14 +245,15 @@ inline int attn_dkv_slices(const AttnArgs& a, size_t max_bytes) {
   return best;
 }
 
-// dK/dV of the sinks from the queries past their window: key blocks of a sequence (0: no query is), and the slices of their walk, a workgroup each: as many as
-// give every CU one, of four steps at least.  Like the others a property of the sizes.
+// dK/dV of the sinks from the queries past their window: key blocks of a sequence (0: no query is), and the slices of their walk, a workgroup each, whose sums
+// meet in scratch (also of one slice: workgroups of the windows, in the same launch, add to the same rows): as many as give every CU one, of four steps at least.  Like
+// the others a property of the sizes.
 inline int attn_sink_blocks(const AttnArgs& a) {
   if (a.sinks == 0 || (int64_t)a.q_start + a.q_len - 1 < (int64_t)a.kv_first + a.window) return 0;
   return (int)cdiv((a.kv_firsts ? ATTN_KV_TILE - 1 : a.kv_first % ATTN_KV_TILE) + (int64_t)a.sinks, ATTN_KV_TILE);
 }
 inline size_t attn_sink_scratch_bytes(const AttnArgs& a, int slices) {      // [sequence][slice][dk | dv][sink][kv head][dh] fp32
-  return slices < 2 ? 0 : (size_t)a.batch * slices * 2 * a.sinks * a.Hkv * a.dh * sizeof(float);
+  return attn_sink_blocks(a) == 0 ? 0 : (size_t)a.batch * slices * 2 * a.sinks * a.Hkv * a.dh * sizeof(float);
 }
 inline int attn_sink_slices(const AttnArgs& a, size_t max_bytes) {
   const int64_t blocks = (int64_t)attn_sink_blocks(a) * a.Hkv * a.batch;
