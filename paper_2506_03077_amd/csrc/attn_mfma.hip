@@ -1648,20 +1648,35 @@ __global__ __launch_bounds__(256) void attn_dkv_sum_sinks_k(const float* __restr
   const int64_t row = (int64_t)Hkv * DH, at = head * DH + e;
   float* out = (is_dk ? dk : dv) + (sq * n_total + key) * row + at;
   f32x4 x = *(const f32x4*)out, y = *(const f32x4*)(out + DH / 2);
-  auto add = [&](const float* src, int n, int64_t step) {
-#pragma unroll 4
-    for (int z = 0; z < n; ++z) {
-      x += *(const f32x4*)(src + z * step);
-      y += *(const f32x4*)(src + z * step + DH / 2);
-    }
-  };
   if (part && key >= first) {
     const int64_t n = (n_total - first) * row;
-    add(part + sq * slices * 2 * n + (is_dk ? 0 : n) + (key - first) * row + at, slices, 2 * n);
+    const float* src = part + sq * slices * 2 * n + (is_dk ? 0 : n) + (key - first) * row + at;
+#pragma unroll 4
+    for (int z = 0; z < slices; ++z) {
+      x += *(const f32x4*)(src + z * 2 * n);
+      y += *(const f32x4*)(src + z * 2 * n + DH / 2);
+    }
   }
-  if (sink_part && key >= kv_first && key < sink_end) {
+  if (sink_part && key >= kv_first && key < sink_end) {      // up to 256 parts of few rows: eight under way at a time
     const int64_t n = sinks * row;
-    add(sink_part + sq * sink_slices * 2 * n + (is_dk ? 0 : n) + (key - kv_first) * row + at, sink_slices, 2 * n);
+    const float* src = sink_part + sq * sink_slices * 2 * n + (is_dk ? 0 : n) + (key - kv_first) * row + at;
+    for (int z0 = 0; z0 < sink_slices; z0 += 8) {
+      f32x4 u[8], w[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        const float* p = src + min(z0 + z, sink_slices - 1) * 2 * n;
+        u[z] = *(const f32x4*)p;
+        w[z] = *(const f32x4*)(p + DH / 2);
+      }
+#pragma unroll
+      for (int z = 0; z < 8; ++z) asm volatile("" : "+v"(u[z]), "+v"(w[z]));      // (all loads before the first sum)
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        const bool in = z0 + z < sink_slices;
+        x = in ? x + u[z] : x;
+        y = in ? y + w[z] : y;
+      }
+    }
   }
   *(f32x4*)out = x;
   *(f32x4*)(out + DH / 2) = y;
