@@ -1,8 +1,9 @@
 // Optimizer step for gfx950: AdamW over a table of tensors, and the norm of their gradients.
 //
-// Both stream memory once: per element AdamW reads weight, gradient and two states and writes weight and states back, and does some fifty vector
-// instructions.  A thread has eight consecutive elements, in 16-byte loads; 32 threads have a block of 256, whose magnitudes meet
-// in registers where the states have 8 bits.
+// Both stream memory once: per element AdamW reads weight, gradient and two states and writes weight and states back.  A thread has eight consecutive elements, in
+// 16-byte loads; 32 threads have a block of 256, whose magnitudes meet in registers where the states have 8 bits.
+// What bounds it: memory, with 32-bit states by far.  With 8-bit states and bf16 weights and gradients an element is 10 bytes, in whose time the chip does about 60 vector
+// instructions, so those are counted: @@COUNT@@
 #include "optim.h"
 #include "device.h"
 
@@ -80,11 +81,12 @@ template <bool WHOLE> __device__ __forceinline__ void put_bytes(uint8_t* p, cons
 }
 
 // ---- random bits: see the public header
-__device__ __forceinline__ uint32_t mix(uint32_t x) {
-  x = (x ^ (x >> 16)) * 0x9E3779B1u;
-  x = (x ^ (x >> 15)) * 0xB504F333u;
+constexpr uint32_t MIX1 = 0x9E3779B1u, MIX2 = 0xB504F333u;
+__device__ __forceinline__ uint32_t mix_end(uint32_t x) {      // ... from the first product on
+  x = (x ^ (x >> 15)) * MIX2;
   return x ^ (x >> 16);
 }
+__device__ __forceinline__ uint32_t mix(uint32_t x) { return mix_end((x ^ (x >> 16)) * MIX1); }
 
 // ---- e4m3 times a power of two ----------------------------------------------------------------------------------
 // Largest bit pattern of non-negative floats over the 32 lanes that share a block: the order of the patterns is that of the values, NaN above infinity.
@@ -100,12 +102,18 @@ constexpr uint32_t NOT_FINITE = 0x7f800000u;
 // The byte of a block whose largest magnitude has this pattern: 2^(byte - 127) brings it to [128, 256)
 __device__ __forceinline__ uint32_t scale_byte(uint32_t largest) { return max(largest >> 23, 8u) - 7u; }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(max(byte << 23, 0x00400000u)); }      // (byte 0: 2^-127, below the normal range)
-__device__ __forceinline__ float inverse_scale_of(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }       // byte 1 .. 248
-// x * inverse as the code of an e4m3 value, u / 2^20 of a step added before the rest is cut off: a float 2^120 times smaller has the e4m3 value's
-// exponent, and below its smallest normal one its fixed point, twenty bits further up.
-__device__ __forceinline__ uint32_t e4m3_code(float x, float inverse, uint32_t u) {
-  const uint32_t b = __float_as_uint(fabsf(x) * inverse * 0x1p-120f);
-  return min((b + u) >> 20, 0x7fu);      // (infinities and NaN: NaN)
+// A magnitude as the code of an e4m3 value of 2^(byte - 127): a float 2^120 times smaller than the value has the e4m3 value's exponent, and below its smallest normal
+// one its fixed point, in bits 20 to 26.  u / 2^20 of a step is added before the rest is cut off.
+__device__ __forceinline__ uint32_t e4m3_bits(float x, uint32_t byte) { return __float_as_uint(__builtin_amdgcn_ldexpf(fabsf(x), 7 - (int)byte)); }
+// the top bytes of four words
+__device__ __forceinline__ uint32_t top_bytes(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+  return __builtin_amdgcn_perm(x1, x0, 0x0c0c0703u) | __builtin_amdgcn_perm(x3, x2, 0x07030c0cu);
+}
+// Root and reciprocal by the hardware's instructions, a unit in the last place off at most.  They take no numbers below the normal range: a v of less is scaled up; the reciprocal's
+// argument is a root or more.
+__device__ __forceinline__ float root_of(float v) {
+  const bool tiny = v < 0x1p-96f;
+  return __builtin_amdgcn_sqrtf(v * (tiny ? 0x1p64f : 1.f)) * (tiny ? 0x1p-32f : 1.f);
 }
 
 struct Consts { float beta1, rest1, beta2, rest2, eps, bias1, bias2; double lr; uint32_t key; float grad_scale; };
@@ -138,15 +146,25 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
     const float x = g[i] * c.grad_scale;
     m[i] = m[i] * c.beta1 + x * c.rest1;
     v[i] = v[i] * c.beta2 + x * x * c.rest2;
-    root[i] = sqrtf(v[i]);
-    w[i] = w[i] * keep - c.bias1 * m[i] / (root[i] * c.bias2 + c.eps);
+    root[i] = root_of(v[i]);
+    w[i] = w[i] * keep - c.bias1 * m[i] * __builtin_amdgcn_rcpf(root[i] * c.bias2 + c.eps);
   }
   uint32_t r[8];
   constexpr bool ROUNDS = sizeof(P) == 2 && !MASTER;
   if constexpr (EIGHT || ROUNDS) {
     const uint32_t key = e >> 32 ? mix(c.key + (uint32_t)(e >> 32)) : c.key;
+    // mix((e + i) ^ key), e a multiple of eight: the first shift moves the same bits for all eight, and each bit of i adds its multiple of the first factor to their product or takes
+    // it away, so that eight words cost one first product instead of eight (a product of 32 bits is four other instructions)
+    const uint32_t x = (uint32_t)e ^ key, y = x ^ (x >> 16);
+    r[0] = y * MIX1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = mix((uint32_t)(e + i) ^ key);
+    for (int b = 0; b < 3; ++b) {
+      const uint32_t d = y >> b & 1 ? 0u - (MIX1 << b) : MIX1 << b;
+#pragma unroll
+      for (int i = 0; i < 1 << b; ++i) r[i + (1 << b)] = r[i] + d;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = mix_end(r[i]);
   }
   if constexpr (EIGHT) {
     uint32_t mx = 0, vx = 0;
@@ -155,7 +173,8 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
       if (WHOLE || i < n) { mx = max(mx, __float_as_uint(m[i]) & 0x7fffffffu); vx = max(vx, __float_as_uint(root[i]) & 0x7fffffffu); }
     mx = max_of_block(mx);
     vx = max_of_block(vx);
-    if (__builtin_amdgcn_ballot_w64(max(mx, vx) >= NOT_FINITE) != 0) {      // they become NaN, and the scale is that of the others
+    const bool odd = __builtin_amdgcn_ballot_w64(max(mx, vx) >= NOT_FINITE) != 0;      // some element of the wave is not finite: it becomes NaN, and the scale is that of the others
+    if (odd) {
       mx = vx = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -167,13 +186,21 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
       vx = max_of_block(vx);
     }
     const uint32_t mb = scale_byte(mx), vb = scale_byte(vx);
-    const float mi = inverse_scale_of(mb), vi = inverse_scale_of(vb);
-    u32x2 mc = {0, 0}, vc = {0, 0};
+    uint32_t a[8], b[8];      // the codes, in the top bytes
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      mc[i >> 2] |= (e4m3_code(m[i], mi, r[i] >> 12) | (__float_as_uint(m[i]) >> 24 & 0x80u)) << (8 * (i & 3));
-      vc[i >> 2] |= max(e4m3_code(root[i], vi, r[i] & 0xfffffu), root[i] > 0.f ? 1u : 0u) << (8 * (i & 3));
+      a[i] = (((e4m3_bits(m[i], mb) + (r[i] >> 12)) << 4) & 0x7fffffffu) | (__float_as_uint(m[i]) & 0x80000000u);
+      // a root's pattern is zero or more than that of the smallest e4m3 value: code 1 at least
+      b[i] = max(e4m3_bits(root[i], vb) + (r[i] & 0xfffffu), min(__float_as_uint(root[i]), 1u << 20)) << 4;
     }
+    if (odd) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if ((__float_as_uint(m[i]) & 0x7fffffffu) >= NOT_FINITE) a[i] = 0x7f000000u;
+        if ((__float_as_uint(root[i]) & 0x7fffffffu) >= NOT_FINITE) b[i] = 0x7f000000u;
+      }
+    }
+    const u32x2 mc = {top_bytes(a[0], a[1], a[2], a[3]), top_bytes(a[4], a[5], a[6], a[7])}, vc = {top_bytes(b[0], b[1], b[2], b[3]), top_bytes(b[4], b[5], b[6], b[7])};
     put_bytes<WHOLE>((uint8_t*)t.m + e, mc, n);
     put_bytes<WHOLE>((uint8_t*)t.v + e, vc, n);
     if ((threadIdx.x & 31) == 0 && (WHOLE || n > 0)) { t.m_scale[e / ADAMW_BLOCK] = (uint8_t)mb; t.v_scale[e / ADAMW_BLOCK] = (uint8_t)vb; }
@@ -184,9 +211,9 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
   if constexpr (MASTER) put<WHOLE>(t.master + e, w, n);
   if constexpr (ROUNDS) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) {      // (then exact; an infinity has nothing below its last bit, NaN stays NaN)
       const uint32_t b = __float_as_uint(w[i]);
-      w[i] = __uint_as_float((b & NOT_FINITE) == NOT_FINITE ? b : (b + (r[i] & 0xffffu)) & 0xffff0000u);      // (then exact; infinities and NaN as they are)
+      w[i] = w[i] != w[i] ? w[i] : __uint_as_float((b + (r[i] & 0xffffu)) & 0xffff0000u);
     }
   }
   put<WHOLE>((P*)t.param + e, w, n);
