@@ -6,9 +6,12 @@ namespace sbp {
 
 constexpr int ADAMW_BLOCK = 256;                            // elements that share the scale of an 8-bit state
 constexpr int ADAMW_TABLE = 40, NORM_TABLE = 128;           // tensors of a launch: what its arguments hold (less than 4 KB)
-constexpr int64_t ADAMW_SPAN = 8192;                        // elements of a workgroup
+// Elements of a workgroup: one pass, without a loop.  In a loop of passes the loads of one wait for the instructions of the one before: this / a loop over 8192 / over 32768, 233 M weights
+// with fp32 states 1158 / 1330 / 1388 us, 545 M with 8-bit states 938 / 1038 / 1084, 237 M of them in 113 tensors 515 / 563 / 611.
+constexpr int64_t ADAMW_SPAN = 2048;
+constexpr int64_t ADAMW_MOST = (int64_t)1 << 34;            // ... of a launch: its threads are counted in 32 bits
 constexpr int NORM_WORKGROUPS = 2048;                       // ... of a norm: that many workgroups, and one more per tensor
-constexpr int64_t NORM_SPAN = 8192;                         // ... of at least so many elements
+constexpr int64_t NORM_SPAN = 8192;                         // ... of at least so many elements, and a multiple of it
 
 struct AdamwTensor {
   int64_t n;
@@ -21,18 +24,19 @@ struct AdamwTensor {
 struct AdamwNow { double lr; int32_t step, pad; };
 struct AdamwArgs {
   double lr, beta1, beta2, eps;
-  float bias1, bias2;          // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  double log1, log2;           // of beta1 and beta2 (-infinity for 0)
+  float bias1, bias2;          // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t), without `now`
   uint32_t seed;
   int32_t step;
   const float* grad_scale;
   const AdamwNow* now;
   int32_t eight, zero_grads;
 };
-// n <= ADAMW_TABLE tensors, first_group filled in here; tensors of no elements are left out by the caller
+// n <= ADAMW_TABLE tensors, ADAMW_MOST elements together, first_group filled in here; tensors of no elements are left out by the caller
 hipError_t adamw_step(const AdamwArgs& a, const AdamwTensor* t, int n, hipStream_t st);
 
 struct NormTensor { const void* grad; int64_t n; uint32_t first_group; int32_t dtype; };
-// Sums of squares of n <= NORM_TABLE tensors, one fp64 for every `span` elements (a multiple of 2048) of a tensor, into part[0 ..]; returns their
+// Sums of squares of n <= NORM_TABLE tensors, one fp64 for every `span` elements (a multiple of NORM_SPAN) of a tensor, into part[0 ..]; returns their
 // number in n_parts
 hipError_t norm_parts(const NormTensor* t, int n, int64_t span, double* part, int* n_parts, hipStream_t st);
 // norm = sqrt(sum of part[0 .. n)), scale (or NULL) = min(1, max_norm / norm)

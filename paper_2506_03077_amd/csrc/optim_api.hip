@@ -23,14 +23,12 @@ static_assert(ADAMW_BLOCK == SBP_STATE_BLOCK, "the block of the public header");
 bool valid_dtype(int dt) { return dt == SBP_F32 || dt == SBP_BF16; }
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 36;      // of all tensors of a call: more than fit a card, and the threads of a launch stay below 2^32
 
 int32_t check_table(int32_t n, const sbp_adamw_tensor* t) {
   if (n < 0) return fail(SBP_ERR_SHAPE, "n_tensors must be >= 0");
   if (n > 0 && !t) return fail(SBP_ERR_NULL, "the table of tensors is NULL");
-  int64_t total = 0;
   for (int i = 0; i < n; ++i) {
-    if (t[i].n < 0 || t[i].n > MOST_ELEMENTS || (total += t[i].n) > MOST_ELEMENTS) return fail(SBP_ERR_SHAPE, "tensor %d: n = %lld, or the sum so far, is outside [0, 2^36]", i, (long long)t[i].n);
+    if (t[i].n < 0 || t[i].n > ADAMW_MOST) return fail(SBP_ERR_SHAPE, "tensor %d: n = %lld is outside [0, 2^34]", i, (long long)t[i].n);
     if (t[i].n == 0) continue;
     if (!valid_dtype(t[i].grad_dtype)) return fail(SBP_ERR_UNSUPPORTED, "tensor %d: grad_dtype %d not supported", i, t[i].grad_dtype);
     if (!t[i].grad) return fail(SBP_ERR_NULL, "tensor %d: grad is NULL", i);
@@ -76,21 +74,29 @@ int32_t streambp_adamw_step(const sbp_adamw_cfg* c, int32_t n_tensors, const sbp
   a.lr = c->lr; a.beta1 = c->beta1; a.beta2 = c->beta2; a.eps = c->eps;
   a.seed = c->seed; a.step = c->step; a.grad_scale = grad_scale; a.now = (const AdamwNow*)now;
   a.eight = c->state == SBP_STATE_8BIT; a.zero_grads = c->zero_grads;
+  a.log1 = std::log(c->beta1); a.log2 = std::log(c->beta2);
   if (!now) {
-    // 1 - b^t by expm1, exact for b next to 1 too; b = 0: 1
-    a.bias1 = (float)(c->lr / (c->beta1 > 0.0 ? -std::expm1(c->step * std::log(c->beta1)) : 1.0));
-    a.bias2 = (float)(1.0 / std::sqrt(c->beta2 > 0.0 ? -std::expm1(c->step * std::log(c->beta2)) : 1.0));
+    // 1 - b^t by expm1, exact for b next to 1 too; b = 0: 1 + expm1(-infinity) of no effect
+    a.bias1 = (float)(c->lr / -std::expm1(c->step * a.log1));
+    a.bias2 = (float)(1.0 / std::sqrt(-std::expm1(c->step * a.log2)));
   }
   AdamwTensor table[ADAMW_TABLE];
   int n = 0;
+  int64_t elements = 0;
+  auto flush = [&]() {
+    const hipError_t e = n > 0 ? adamw_step(a, table, n, (hipStream_t)hip_stream) : hipSuccess;
+    n = 0;
+    elements = 0;
+    return e;
+  };
   for (int i = 0; i < n_tensors; ++i) {
     const sbp_adamw_tensor& x = tensors[i];
-    if (x.n > 0) table[n++] = AdamwTensor{x.n, x.weight_decay, x.param, x.master, x.grad, x.m, x.v, (uint8_t*)x.m_scale, (uint8_t*)x.v_scale, 0, (uint32_t)i, x.dtype, x.grad_dtype};
-    if (n == ADAMW_TABLE || (i == n_tensors - 1 && n > 0)) {
-      HIPCHK(adamw_step(a, table, n, (hipStream_t)hip_stream));
-      n = 0;
-    }
+    if (x.n == 0) continue;
+    if (n == ADAMW_TABLE || elements + x.n > ADAMW_MOST) HIPCHK(flush());
+    table[n++] = AdamwTensor{x.n, x.weight_decay, x.param, x.master, x.grad, x.m, x.v, (uint8_t*)x.m_scale, (uint8_t*)x.v_scale, 0, (uint32_t)i, x.dtype, x.grad_dtype};
+    elements += x.n;
   }
+  HIPCHK(flush());
   return SBP_OK;
 }
 
@@ -109,7 +115,7 @@ int32_t streambp_grad_norm(int32_t n_tensors, const sbp_adamw_tensor* tensors, f
   int64_t total = 0;
   for (int i = 0; i < n_tensors; ++i) total += tensors[i].n;
   // (every tensor has at most one span that is not full: no more than NORM_WORKGROUPS + n_tensors of them)
-  const int64_t span = std::max<int64_t>(NORM_SPAN, align_up((size_t)cdiv(total, NORM_WORKGROUPS), 2048));
+  const int64_t span = std::max<int64_t>(NORM_SPAN, align_up((size_t)cdiv(total, NORM_WORKGROUPS), NORM_SPAN));
   NormTensor table[NORM_TABLE];
   int n = 0, parts = 0;
   for (int i = 0; i < n_tensors; ++i) {

@@ -34,7 +34,7 @@ NULL, SHAPE, UNSUPPORTED, WORKSPACE = -1, -2, -3, -4
     (NULL, None, {}), (UNSUPPORTED, cfg(state=2), {}), (SHAPE, cfg(step=0), {}), (SHAPE, cfg(lr=-1.0), {}), (SHAPE, cfg(lr=float("nan")), {}),
     (SHAPE, cfg(lr=float("inf")), {}), (SHAPE, cfg(beta1=1.0), {}), (SHAPE, cfg(beta2=-0.1), {}), (SHAPE, cfg(beta2=float("nan")), {}),
     (SHAPE, cfg(eps=-1e-8), {}), (SHAPE, cfg(eps=float("inf")), {}), (SHAPE, cfg(zero_grads=2), {}),
-    (SHAPE, cfg(), dict(n=-1)), (SHAPE, cfg(), dict(n=2 ** 36 + 1)), (SHAPE, cfg(), dict(weight_decay=-0.1)), (SHAPE, cfg(), dict(weight_decay=float("nan"))),
+    (SHAPE, cfg(), dict(n=-1)), (SHAPE, cfg(), dict(n=2 ** 34 + 1)), (SHAPE, cfg(), dict(weight_decay=-0.1)), (SHAPE, cfg(), dict(weight_decay=float("nan"))),
     (UNSUPPORTED, cfg(), dict(dtype=2)), (UNSUPPORTED, cfg(), dict(grad_dtype=7)), (UNSUPPORTED, cfg(), dict(dtype=sb.SBP_F32, master=P)),
     (NULL, cfg(), dict(param=None)), (NULL, cfg(), dict(grad=None)), (NULL, cfg(), dict(m=None)), (NULL, cfg(), dict(v=None)),
     (NULL, cfg(state=1), {}), (NULL, cfg(state=1), dict(m_scale=P)), (UNSUPPORTED, cfg(), dict(m_scale=P, v_scale=P)),
@@ -51,8 +51,6 @@ def test_adamw_refuses_odd_scalars_and_counts():
     assert call(cfg(), [tensor()], now=P + 4) == UNSUPPORTED
     assert sb.lib().streambp_adamw_step(C.byref(cfg()), -1, None, None, None, None) == SHAPE
     assert sb.lib().streambp_adamw_step(C.byref(cfg()), 1, None, None, None, None) == NULL
-    many = [tensor(n=2 ** 35)] * 3                # together more than 2^36
-    assert call(cfg(), many) == SHAPE
 
 
 def test_nothing_to_do_is_no_error():
