@@ -10,7 +10,7 @@ resident in HBM.  Prints ONE JSON line (see README for the fields).
 
     python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload 7b|llama_layer|lmhead|grpo|stack] [--seq-len T]
                     [--chunk C] [--batch B] [--prompt-frac P] [--layers L] [--grad-dtype f32|bf16] [--no-cpu-baseline]
-                    [--no-profile]
+                    [--no-profile] [--window W [--sinks S]] [--optimizer none|adamw|adamw8]
 """
 from __future__ import annotations
 
@@ -37,7 +37,7 @@ MEASURED_TRAFFIC = {      # kernel symbol -> (bytes per launch, file under profi
 }
 
 
-def algorithmic_flops(cfg, T, active_rows, batch=1, has_layer=True, has_head=True, n_layers=1, lora_rank=0, window=0):
+def algorithmic_flops(cfg, T, active_rows, batch=1, has_layer=True, has_head=True, n_layers=1, lora_rank=0, window=0, sinks=0):
     """Work the method must do (Sec. 3.2): 6*P per token for the linear maps (reforward, dX, dW), 14*dh per
     visible causal (query, key) pair per query head (4 forward + 10 backward), 6*d*V per row of the head.
     T = tokens per sequence, batch sequences (no attention across sequences), active_rows over the whole batch."""
@@ -53,6 +53,8 @@ def algorithmic_flops(cfg, T, active_rows, batch=1, has_layer=True, has_head=Tru
         pairs = T * (T + 1) / 2.0
         if window and window < T:                                              # visible (query, key) pairs under a sliding window
             pairs = window * (window + 1) / 2.0 + (T - window) * float(window)
+            s = min(sinks, T - window)                                         # ... and of its queries past the window with the sinks
+            pairs += s * (s + 1) / 2.0 + (T - window - s) * float(s)
         attn = 14.0 * dh * Hq * pairs * batch * n_layers
     if has_head:
         V = cfg["vocab"]
@@ -114,6 +116,10 @@ def main():
                     help="7b / llama_layer / grpo: run the layer in adapter mode (rank-R adapters on all seven matrices, adapter "
                          "gradients only; the paper's setting for its largest model is R = 32)")
     ap.add_argument("--window", type=int, default=0, help="sliding-window attention in the layer (0 = plain causal)")
+    ap.add_argument("--sinks", type=int, default=0, help="first tokens of a sequence that stay visible behind the window")
+    ap.add_argument("--optimizer", choices=("none", "adamw", "adamw8"), default="none",
+                    help="after the timed steps, time the norm of all gradients and an AdamW step over all weights (adapters in adapter mode), "
+                         "reported in config.optimizer: adamw = 32-bit states and fp32 master copies, adamw8 = 8-bit states, no copies")
     ap.add_argument("--grad-dtype", choices=("f32", "bf16"), default="f32",
                     help="element type of the weight-gradient accumulators (default fp32; bf16 is the paper's own training "
                          "setting, App. D (experiment setup), and halves the read-modify-write traffic on dW)")
@@ -167,7 +173,7 @@ def main():
     prompt_frac = args.prompt_frac if args.prompt_frac is not None else (0.25 if wl in ("lmhead", "grpo") else 0.0)
     gdt = sb.SBP_BF16 if args.grad_dtype == "bf16" else sb.SBP_F32
     default_shape = (wl == "7b" and T == cfg["seq_len"] and c == cfg["chunk"] and hc_rows == c and B == cfg["batch"]
-                     and not args.lora_rank and not args.window and prompt_frac == 0.0 and gdt == sb.SBP_F32 and args.dw_group_rows == 0)   # what the profiles cover
+                     and not args.lora_rank and not args.window and not args.sinks and prompt_frac == 0.0 and gdt == sb.SBP_F32 and args.dw_group_rows == 0)   # what the profiles cover
     d = cfg["hidden"]
     bf = torch.bfloat16
 
@@ -194,7 +200,7 @@ def main():
     if has_layer:
         Hq, Hkv, dh, F = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"], cfg["mlp_width"]
         lcfg = sb.layer_cfg(sb.SBP_BF16, B, T, c, d, Hq, Hkv, dh, F, grad_dtype=gdt, dw_group_rows=args.dw_group_rows,
-                            window=args.window)
+                            window=args.window, sinks=args.sinks)
         assert sb.streambp_layer_fast_path(lcfg) == 1, sb.streambp_last_error()
         ws_bytes["layer_workspace"] = sb.streambp_layer_workspace_bytes(lcfg)
     if has_head:
@@ -239,7 +245,10 @@ def main():
         def step():
             sb.streambp_stack_backward(scfg, layers, g_final, w_head, ckpt, targets, ids=ids, workspace=ws_stack, **grads)
         dx = grads["dx0"]
+        trained = [(w[n], dw[n]) for w, dw in zip(layers, grads["dlayers"]) for n in sb.WEIGHT_NAMES]
+        trained += [(g_final, grads["dg_final"]), (w_head, dw_head), (emb, grads["demb"])]
     else:
+        trained = []
         if has_layer:
             w = layer_weights()
             x = normal((B, T, d), 1.0)          # layer input (the checkpoint)
@@ -252,10 +261,12 @@ def main():
             ws_layer = torch.empty(ws_bytes["layer_workspace"], dtype=torch.uint8, device=dev)
             dw = sb.new_layer_grads(w, gdt)
             dx = torch.empty_like(x)
+            trained += [p for n in sb.MATRIX_NAMES for p in zip(adapters[n], (da[n], db[n]))] if args.lora_rank else [(w[n], dw[n]) for n in sb.WEIGHT_NAMES]
         if has_head:
             h = normal((B, T, d), 1.0)          # hidden states entering the head
             ws_head = torch.empty(ws_bytes["head_workspace"], dtype=torch.uint8, device=dev)
             dh_out = torch.empty_like(h)
+            trained.append((w_head, dw_head))
         else:
             dh_out = normal((B, T, d), 1e-3)    # upstream gradient of the layer
 
@@ -299,7 +310,7 @@ def main():
     if has_layer:
         assert bool(torch.isfinite(dx.float()).all())
 
-    fl = algorithmic_flops(cfg, T, n_act, B, has_layer, has_head, L, args.lora_rank, args.window)
+    fl = algorithmic_flops(cfg, T, n_act, B, has_layer, has_head, L, args.lora_rank, args.window, args.sinks)
     names = {"7b": "7B-shaped decoder layer (d=3584, 28q/4kv x128, F=18944) + LM head (V=152064)",
              "llama_layer": "Llama-style decoder layer (d=4096, 32q/8kv x128, F=14336), upstream gradient N(0,1e-3)",
              "lmhead": "LM head + cross-entropy (d=3584, V=152064)",
@@ -317,6 +328,7 @@ def main():
                                f"{args.grad_dtype} weight-gradient accumulators"
                                + (f", layer in adapter mode (rank {args.lora_rank} on all seven matrices, adapter gradients only)" if args.lora_rank else "")
                                + (f", sliding window {args.window}" if args.window else "")
+                               + (f", {args.sinks} sinks" if args.sinks else "")
                                + (f", weight gradients added once per {args.dw_group_rows} rows" if args.dw_group_rows else ""),
                    "algorithmic_tflop_per_step": fl["total"] / 1e12,
                    "achieved_tflops": fl["total"] / dt / 1e12,
@@ -372,6 +384,35 @@ def main():
         out["config"]["same_step_with_first_25pct_of_positions_ignored"] = dict(
             ms_per_step=dt2 * 1e3, tokens_per_s=B * T / dt2, algorithmic_tflop_per_step=fl2["total"] / 1e12,
             achieved_tflops=fl2["total"] / dt2 / 1e12, frac_of_bf16_mfma_peak=fl2["total"] / dt2 / 1e12 / PEAK_BF16_TFLOPS)
+    # ---- the step that follows the backward: norm of all gradients, then AdamW with the factor that limits it, gradients cleared.
+    if args.optimizer != "none":
+        eight = args.optimizer == "adamw8"
+        state = sb.SBP_STATE_8BIT if eight else sb.SBP_STATE_F32
+        table = sb.adamw_tensors([dict(sb.new_adamw_states(p, state, master=not eight), grad=g, weight_decay=0.0 if p.dim() == 1 else 0.1) for p, g in trained])
+        ws_norm = torch.empty(sb.streambp_grad_norm_workspace_bytes(len(table)), dtype=torch.uint8, device=dev)
+        norm, factor = (torch.empty(1, dtype=torch.float32, device=dev) for _ in range(2))
+        ms = {"grad_norm": [], "adamw": []}
+        for t in range(1, args.steps + 2):                # the first one untimed
+            step()
+            events = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
+            events[0].record()
+            sb.streambp_grad_norm(table, 1.0, norm=norm, grad_scale=factor, workspace=ws_norm)
+            events[1].record()
+            sb.streambp_adamw_step(sb.adamw_cfg(1e-5, beta2=0.95, step=t, state=state, zero_grads=True), table, grad_scale=factor)
+            events[2].record()
+            torch.cuda.synchronize()
+            assert bool(torch.isfinite(norm).all())
+            if t > 1:
+                ms["grad_norm"].append(events[0].elapsed_time(events[1]))
+                ms["adamw"].append(events[1].elapsed_time(events[2]))
+        held = sum(t[n].numel() * t[n].element_size() for t in table.tensors for n in ("m", "v", "master", "m_scale", "v_scale") if n in t)
+        read = sum(g.numel() * g.element_size() for _, g in trained)
+        weights = sum(p.numel() * p.element_size() for p, _ in trained)
+        ms = {n: sum(v) / len(v) for n, v in ms.items() if v}
+        out["config"]["optimizer"] = dict(
+            kind=args.optimizer, elements=sum(p.numel() for p, _ in trained), tensors=len(trained), states_bytes=held, last_grad_norm=float(norm.item()),
+            ms=ms, gb_per_s={} if not ms else {"grad_norm": read / ms["grad_norm"] / 1e6,
+                                               "adamw": (2 * read + 2 * held + weights * (2 if eight else 1)) / ms["adamw"] / 1e6})
     # ---- context for the roofline fractions: what the matrix pipe sustains with NO global memory traffic at all (eight
     # independent MFMAs per wave and round, two waves per SIMD).  The chip is power-managed, so the rate depends on the operand
     # values: all-zero fragments reach the nominal peak, random ones (what every GEMM of the path multiplies) do not - and

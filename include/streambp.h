@@ -392,7 +392,7 @@ typedef struct {
                            before the next backward                                  */
 } sbp_adamw_cfg;
 
-/* One tensor: n >= 0 elements, dense, in any order that its parts share (n = 0: the pointers are not read).  Tensors of a call
+/* One tensor: 0 <= n <= 2^34 elements, dense, in any order that its parts share (n = 0: the pointers are not read).  Tensors of a call
  * may not overlap.  Pointers need the alignment of their elements; where param, master, grad, m and v are 16-byte aligned (8-bit m, v: 8) the
  * step is as fast as memory, otherwise several times slower. */
 typedef struct {
