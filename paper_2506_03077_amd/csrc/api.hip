@@ -374,9 +374,9 @@ AttnArgs pass_attn(const sbp_layer_cfg* c, const LayerWs& s, const Pass& p) {
   AttnArgs aa{};
   aa.dt = c->dtype; aa.Hq = c->n_q_heads; aa.Hkv = c->n_kv_heads; aa.dh = c->head_dim;
   aa.batch = p.seqs; aa.q_start = p.r0; aa.q_len = p.n; aa.scale = 1.0f / std::sqrt((float)c->head_dim);
-  aa.window = c->window; aa.kv_first = c->seq_first ? *std::min_element(c->seq_first + p.b0, c->seq_first + p.b0 + p.seqs) : 0;      // rows before it are padding in front of the sequence
+  aa.kv_first = c->seq_first ? *std::min_element(c->seq_first + p.b0, c->seq_first + p.b0 + p.seqs) : 0;      // rows before it are padding in front of the sequence
   aa.kv_firsts = c->seq_first && p.seqs > 1 ? c->seq_first + p.b0 : nullptr;
-  attn_set_sinks(aa, c->sinks);
+  attn_set_window(aa, c->window, c->sinks);
   aa.q = s.q; aa.k = s.K; aa.v = s.V; aa.o = s.o; aa.lse = s.lse;
   if (fusion_mask() & FUSE_ROPE_Q) aa.rope_q = s.rope + (size_t)p.r0 * (c->head_dim / 2);
   return aa;
@@ -1035,8 +1035,8 @@ static size_t attn_stats_bytes(const sbp_attn_cfg* c) { return align_up((size_t)
 static AttnArgs attn_args(const sbp_attn_cfg* c) {
   AttnArgs a{};
   a.dt = c->dtype; a.Hq = c->n_q_heads; a.Hkv = c->n_kv_heads; a.dh = c->head_dim;
-  a.q_start = c->q_start; a.q_len = c->q_len; a.scale = c->scale; a.window = c->window; a.kv_first = c->kv_first;
-  attn_set_sinks(a, c->sinks);
+  a.q_start = c->q_start; a.q_len = c->q_len; a.scale = c->scale; a.kv_first = c->kv_first;
+  attn_set_window(a, c->window, c->sinks);
   if (c->dtype == SBP_BF16 && (c->head_dim == 128 || c->head_dim == 64)) {
     a.dkv_slices = attn_dkv_slices(a, SIZE_MAX);
     a.sink_slices = attn_sink_slices(a, SIZE_MAX);

@@ -177,9 +177,9 @@ struct AttnArgs {
   int Hq, Hkv, dh;
   int q_start, q_len;
   float scale;
-  int window = 0;          // > 0: a query at position t sees only keys t - window < u <= t
+  int window = 0;          // > 0: a query at position t sees only keys t - window < u <= t; at most all keys (attn_set_window)
   int kv_first = 0;        // key positions before this one are padding: never visible
-  int sinks = 0;           // the first `sinks` keys from kv_first on stay visible to every later query; 0 without a window, at most all keys (attn_set_sinks)
+  int sinks = 0;           // the first `sinks` keys from kv_first on stay visible to every later query; 0 without a window, at most all keys (attn_set_window)
   // Several sequences in one call, up to ATTN_MAX_SEQS: `batch` of q_len queries and keys each, one behind the other (q_start = 0; lse [batch, Hq, c],
   // delta [batch, 2, Hq, c]), kv_firsts their kv_first on the host (or NULL: kv_first for all; else kv_first is the least of them).
   int batch = 1;
@@ -263,8 +263,9 @@ inline int attn_sink_slices(const AttnArgs& a, size_t max_bytes) {
   while (s > 1 && attn_sink_scratch_bytes(a, (int)s) > max_bytes) --s;
   return (int)s;
 }
-// what a caller's `sinks` come to
-inline void attn_set_sinks(AttnArgs& a, int sinks) {
+// What a caller's window and sinks come to: no more than all keys (positions plus a window are 32-bit sums in the kernels)
+inline void attn_set_window(AttnArgs& a, int window, int sinks) {
+  a.window = std::min(window, a.q_start + a.q_len);
   a.sinks = a.window > 0 ? (int)std::min<int64_t>(sinks, std::max<int64_t>(0, (int64_t)a.q_start + a.q_len - a.kv_first)) : 0;
 }
 
