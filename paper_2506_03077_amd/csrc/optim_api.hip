@@ -20,15 +20,18 @@ namespace {
 static_assert(sizeof(AdamwNow) == sizeof(sbp_adamw_now), "the device's view of sbp_adamw_now");
 static_assert(ADAMW_BLOCK == SBP_STATE_BLOCK, "the block of the public header");
 
+constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 44;
+
 bool valid_dtype(int dt) { return dt == SBP_F32 || dt == SBP_BF16; }
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
 
 int32_t check_table(int32_t n, const sbp_adamw_tensor* t) {
   if (n < 0) return fail(SBP_ERR_SHAPE, "n_tensors must be >= 0");
   if (n > 0 && !t) return fail(SBP_ERR_NULL, "the table of tensors is NULL");
+  int64_t total = 0;      // (more than any memory: the sums of workgroups below stay far from their types' ends)
   for (int i = 0; i < n; ++i) {
     if (t[i].n < 0 || t[i].n > ADAMW_MOST) return fail(SBP_ERR_SHAPE, "tensor %d: n = %lld is outside [0, 2^34]", i, (long long)t[i].n);
+    if ((total += t[i].n) > MOST_ELEMENTS) return fail(SBP_ERR_SHAPE, "tensor %d: more than 2^44 elements together", i);
     if (t[i].n == 0) continue;
     if (!valid_dtype(t[i].grad_dtype)) return fail(SBP_ERR_UNSUPPORTED, "tensor %d: grad_dtype %d not supported", i, t[i].grad_dtype);
     if (!t[i].grad) return fail(SBP_ERR_NULL, "tensor %d: grad is NULL", i);
