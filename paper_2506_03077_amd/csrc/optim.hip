@@ -4,8 +4,8 @@
 // 16-byte loads; 32 threads have a block of 256, whose magnitudes meet in registers where the states have 8 bits.
 // What bounds it: memory, with 32-bit states by far.  With 8-bit states and bf16 weights and gradients an element is 10 bytes, in whose time the chip does about 60 vector
 // instructions, so those are counted: 86 in the first form of this kernel, with the library's root and quotient, about 46 now.
-// Measured: 233 M elements with fp32 states and master copies 1158 us, 6.4 TB/s (a large copy runs at 4.8 TB/s); 545 M with 8-bit states 938 us, 5.8 TB/s.
-// The norm reads 933 MB of fp32 gradients in 155 us and 477 MB of bf16 ones in 84 us, 6.0 and 5.7 TB/s.
+// Measured: 233 M elements with fp32 states and master copies 1335 us, 5.6 TB/s of the bytes above (a large copy runs at 4.8 TB/s); 545 M with 8-bit states 905 us, 6.0 TB/s.
+// The norm reads 933 MB of fp32 gradients in 155 us and 477 MB of bf16 ones in 78 us, 6.0 and 6.1 TB/s.
 #include "optim.h"
 #include "device.h"
 
@@ -36,47 +36,54 @@ __device__ __forceinline__ int tensor_of(const Table& table, uint32_t group) {
 
 // ---- eight elements ---------------------------------------------------------------------------------------------
 // WHOLE: all eight exist and their address is a multiple of 16 (bytes: 8); else `n` of them, element by element.
-__device__ __forceinline__ void load8(float (&x)[8], const float* p) {
-  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+// PAST: what passes the caches by, because it is more than they hold until it is read again (OPTIM_PAST).
+template <bool PAST, typename T> __device__ __forceinline__ T load(const T* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load(p); else return *p;
+}
+template <bool PAST, typename T> __device__ __forceinline__ void store(T* p, T x) {
+  if constexpr (PAST) __builtin_nontemporal_store(x, p); else *p = x;
+}
+template <bool PAST> __device__ __forceinline__ void load8(float (&x)[8], const float* p) {
+  const f32x4 a = load<PAST>((const f32x4*)p), b = load<PAST>((const f32x4*)(p + 4));
 #pragma unroll
   for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
 }
-__device__ __forceinline__ void load8(float (&x)[8], const bf16_t* p) {
-  const u32x4 a = *(const u32x4*)p;
+template <bool PAST> __device__ __forceinline__ void load8(float (&x)[8], const bf16_t* p) {
+  const u32x4 a = load<PAST>((const u32x4*)p);
 #pragma unroll
   for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(a[i] << 16); x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u); }
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
-  *(f32x4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+template <bool PAST> __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  store<PAST>((f32x4*)p, f32x4{x[0], x[1], x[2], x[3]});
+  store<PAST>((f32x4*)(p + 4), f32x4{x[4], x[5], x[6], x[7]});
 }
-__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {      // to nearest
+template <bool PAST> __device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {      // to nearest
   bf16x8 a;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = (bf16_t)x[i];
-  *(bf16x8*)p = a;
+  store<PAST>((bf16x8*)p, a);
 }
-template <bool WHOLE, typename T> __device__ __forceinline__ void get(float (&x)[8], const T* p, int n) {
-  if constexpr (WHOLE) { load8(x, p); return; }
+template <bool WHOLE, bool PAST, typename T> __device__ __forceinline__ void get(float (&x)[8], const T* p, int n) {
+  if constexpr (WHOLE) { load8<PAST>(x, p); return; }
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = i < n ? ldf(p + i) : 0.f;
 }
-template <bool WHOLE, typename T> __device__ __forceinline__ void put(T* p, const float (&x)[8], int n) {
-  if constexpr (WHOLE) { store8(p, x); return; }
+template <bool WHOLE, bool PAST, typename T> __device__ __forceinline__ void put(T* p, const float (&x)[8], int n) {
+  if constexpr (WHOLE) { store8<PAST>(p, x); return; }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (i < n) stf(p + i, x[i]);
 }
-template <bool WHOLE> __device__ __forceinline__ u32x2 get_bytes(const uint8_t* p, int n) {
-  if constexpr (WHOLE) return *(const u32x2*)p;
+template <bool WHOLE, bool PAST> __device__ __forceinline__ u32x2 get_bytes(const uint8_t* p, int n) {
+  if constexpr (WHOLE) return load<PAST>((const u32x2*)p);
   u32x2 w = {0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
   return w;
 }
-template <bool WHOLE> __device__ __forceinline__ void put_bytes(uint8_t* p, const u32x2& w, int n) {
-  if constexpr (WHOLE) { *(u32x2*)p = w; return; }
+template <bool WHOLE, bool PAST> __device__ __forceinline__ void put_bytes(uint8_t* p, const u32x2& w, int n) {
+  if constexpr (WHOLE) { store<PAST>((u32x2*)p, w); return; }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (i < n) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
@@ -120,13 +127,13 @@ __device__ __forceinline__ float root_of(float v) {
 
 struct Consts { float beta1, rest1, beta2, rest2, eps, bias1, bias2; double lr; uint32_t key; float grad_scale; };
 
-template <bool WHOLE, typename P, bool MASTER, typename G, bool EIGHT>
+template <bool WHOLE, typename P, bool MASTER, typename G, bool EIGHT, bool PAST>
 __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Consts& c, float keep, int64_t e, int n, bool zero) {
   float g[8], w[8], m[8], v[8];
-  if constexpr (MASTER) get<WHOLE>(w, t.master + e, n); else get<WHOLE>(w, (const P*)t.param + e, n);
-  get<WHOLE>(g, (const G*)t.grad + e, n);
+  if constexpr (MASTER) get<WHOLE, PAST>(w, t.master + e, n); else get<WHOLE, PAST>(w, (const P*)t.param + e, n);
+  get<WHOLE, PAST>(g, (const G*)t.grad + e, n);
   if constexpr (EIGHT) {
-    const u32x2 mb = get_bytes<WHOLE>((const uint8_t*)t.m + e, n), vb = get_bytes<WHOLE>((const uint8_t*)t.v + e, n);
+    const u32x2 mb = get_bytes<WHOLE, PAST>((const uint8_t*)t.m + e, n), vb = get_bytes<WHOLE, PAST>((const uint8_t*)t.v + e, n);
     const bool in = WHOLE || n > 0;
     const float ms = in ? scale_of(t.m_scale[e / ADAMW_BLOCK]) : 0.f, vs = in ? scale_of(t.v_scale[e / ADAMW_BLOCK]) : 0.f;
 #pragma unroll
@@ -139,8 +146,8 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= v[i];
   } else {
-    get<WHOLE>(m, (const float*)t.m + e, n);
-    get<WHOLE>(v, (const float*)t.v + e, n);
+    get<WHOLE, PAST>(m, (const float*)t.m + e, n);
+    get<WHOLE, PAST>(v, (const float*)t.v + e, n);
   }
   float root[8];
 #pragma unroll
@@ -203,14 +210,14 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
       }
     }
     const u32x2 mc = {top_bytes(a[0], a[1], a[2], a[3]), top_bytes(a[4], a[5], a[6], a[7])}, vc = {top_bytes(b[0], b[1], b[2], b[3]), top_bytes(b[4], b[5], b[6], b[7])};
-    put_bytes<WHOLE>((uint8_t*)t.m + e, mc, n);
-    put_bytes<WHOLE>((uint8_t*)t.v + e, vc, n);
+    put_bytes<WHOLE, PAST>((uint8_t*)t.m + e, mc, n);
+    put_bytes<WHOLE, PAST>((uint8_t*)t.v + e, vc, n);
     if ((threadIdx.x & 31) == 0 && (WHOLE || n > 0)) { t.m_scale[e / ADAMW_BLOCK] = (uint8_t)mb; t.v_scale[e / ADAMW_BLOCK] = (uint8_t)vb; }
   } else {
-    put<WHOLE>((float*)t.m + e, m, n);
-    put<WHOLE>((float*)t.v + e, v, n);
+    put<WHOLE, PAST>((float*)t.m + e, m, n);
+    put<WHOLE, PAST>((float*)t.v + e, v, n);
   }
-  if constexpr (MASTER) put<WHOLE>(t.master + e, w, n);
+  if constexpr (MASTER) put<WHOLE, PAST>(t.master + e, w, n);
   if constexpr (ROUNDS) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {      // (then exact; an infinity has nothing below its last bit, NaN stays NaN)
@@ -218,14 +225,14 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
       w[i] = w[i] != w[i] ? w[i] : __uint_as_float((b + (r[i] & 0xffffu)) & 0xffff0000u);
     }
   }
-  put<WHOLE>((P*)t.param + e, w, n);
+  put<WHOLE, PAST>((P*)t.param + e, w, n);
   if (zero) {
     const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    put<WHOLE>((G*)t.grad + e, none, n);
+    put<WHOLE, PAST>((G*)t.grad + e, none, n);
   }
 }
 
-template <typename P, bool MASTER, typename G, bool EIGHT>
+template <typename P, bool MASTER, typename G, bool EIGHT, bool PAST>
 __device__ __forceinline__ void span_of(const AdamwTensor& t, const Consts& c, int64_t first, bool zero) {
   auto whole16 = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
   auto whole8 = [](const void* p) { return ((uintptr_t)p & 7) == 0; };
@@ -233,11 +240,11 @@ __device__ __forceinline__ void span_of(const AdamwTensor& t, const Consts& c, i
   const float keep = (float)(1.0 - c.lr * t.weight_decay);
   static_assert(ADAMW_SPAN == TILE, "one pass");
   const int64_t e = first + threadIdx.x * PER;
-  if (aligned && first + TILE <= t.n) eight_elements<true, P, MASTER, G, EIGHT>(t, c, keep, e, PER, zero);
-  else eight_elements<false, P, MASTER, G, EIGHT>(t, c, keep, e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)), zero);
+  if (aligned && first + TILE <= t.n) eight_elements<true, P, MASTER, G, EIGHT, PAST>(t, c, keep, e, PER, zero);
+  else eight_elements<false, P, MASTER, G, EIGHT, PAST>(t, c, keep, e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)), zero);
 }
 
-template <bool EIGHT>
+template <bool EIGHT, bool PAST>
 __global__ __launch_bounds__(THREADS) void adamw_k(const AdamwTable table) {
   const AdamwArgs& a = table.a;
   const AdamwTensor& t = table.t[tensor_of(table, blockIdx.x)];
@@ -271,9 +278,9 @@ __global__ __launch_bounds__(THREADS) void adamw_k(const AdamwTable table) {
     return;
   }
   const bool gb = t.grad_dtype == DT_BF16;
-  if (t.dtype == DT_F32) { if (gb) span_of<float, false, bf16_t, EIGHT>(t, c, first, zero); else span_of<float, false, float, EIGHT>(t, c, first, zero); }
-  else if (t.master) { if (gb) span_of<bf16_t, true, bf16_t, EIGHT>(t, c, first, zero); else span_of<bf16_t, true, float, EIGHT>(t, c, first, zero); }
-  else { if (gb) span_of<bf16_t, false, bf16_t, EIGHT>(t, c, first, zero); else span_of<bf16_t, false, float, EIGHT>(t, c, first, zero); }
+  if (t.dtype == DT_F32) { if (gb) span_of<float, false, bf16_t, EIGHT, PAST>(t, c, first, zero); else span_of<float, false, float, EIGHT, PAST>(t, c, first, zero); }
+  else if (t.master) { if (gb) span_of<bf16_t, true, bf16_t, EIGHT, PAST>(t, c, first, zero); else span_of<bf16_t, true, float, EIGHT, PAST>(t, c, first, zero); }
+  else { if (gb) span_of<bf16_t, false, bf16_t, EIGHT, PAST>(t, c, first, zero); else span_of<bf16_t, false, float, EIGHT, PAST>(t, c, first, zero); }
 }
 
 hipError_t adamw_step(const AdamwArgs& a, const AdamwTensor* t, int n, hipStream_t st) {
@@ -287,8 +294,9 @@ hipError_t adamw_step(const AdamwArgs& a, const AdamwTensor* t, int n, hipStream
     table.t[i].first_group = (uint32_t)groups;
     groups += cdiv(t[i].n, ADAMW_SPAN);
   }
-  if (a.eight) adamw_k<true><<<(unsigned)groups, THREADS, 0, st>>>(table);
-  else adamw_k<false><<<(unsigned)groups, THREADS, 0, st>>>(table);
+  if (a.eight && a.past) adamw_k<true, true><<<(unsigned)groups, THREADS, 0, st>>>(table);
+  else if (a.eight) adamw_k<true, false><<<(unsigned)groups, THREADS, 0, st>>>(table);
+  else adamw_k<false, false><<<(unsigned)groups, THREADS, 0, st>>>(table);
   return hipGetLastError();
 }
 
@@ -310,7 +318,7 @@ __device__ __forceinline__ double group_sum(double v) {      // of N threads, th
   return s;
 }
 
-template <typename G>
+template <bool PAST, typename G>
 __device__ __forceinline__ double squares(const NormTensor& t, int64_t first, int64_t span) {
   const G* g = (const G*)t.grad;
   const bool aligned = ((uintptr_t)g & 15) == 0;
@@ -327,26 +335,27 @@ __device__ __forceinline__ double squares(const NormTensor& t, int64_t first, in
   for (; aligned && at + NORM_SPAN <= end; at += NORM_SPAN) {
     float x[DEEP][8];
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i) get<true>(x[i], g + at + i * TILE + threadIdx.x * PER, PER);
+    for (int i = 0; i < DEEP; ++i) get<true, PAST>(x[i], g + at + i * TILE + threadIdx.x * PER, PER);
 #pragma unroll
     for (int i = 0; i < DEEP; ++i) add(x[i]);
   }
   for (; at < end; at += TILE) {
     const int64_t e = at + threadIdx.x * PER;
     float x[8];
-    if (aligned && at + TILE <= t.n) get<true>(x, g + e, PER);
-    else get<false>(x, g + e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)));
+    if (aligned && at + TILE <= t.n) get<true, PAST>(x, g + e, PER);
+    else get<false, PAST>(x, g + e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)));
     add(x);
   }
   return sum;
 }
+template <bool PAST>
 __global__ __launch_bounds__(THREADS) void grad_squares_k(const NormTable table) {
   const NormTensor& t = table.t[tensor_of(table, blockIdx.x)];
   const int64_t first = (int64_t)(blockIdx.x - t.first_group) * table.span;
-  const double s = group_sum<THREADS>(t.dtype == DT_BF16 ? squares<bf16_t>(t, first, table.span) : squares<float>(t, first, table.span));
+  const double s = group_sum<THREADS>(t.dtype == DT_BF16 ? squares<PAST, bf16_t>(t, first, table.span) : squares<PAST, float>(t, first, table.span));
   if (threadIdx.x == 0) table.part[blockIdx.x] = s;
 }
-hipError_t norm_parts(const NormTensor* t, int n, int64_t span, double* part, int* n_parts, hipStream_t st) {
+hipError_t norm_parts(const NormTensor* t, int n, int64_t span, bool past, double* part, int* n_parts, hipStream_t st) {
   if (n < 1 || n > NORM_TABLE || span < NORM_SPAN || span % NORM_SPAN) return hipErrorInvalidValue;
   NormTable table{};
   table.part = part;
@@ -358,7 +367,8 @@ hipError_t norm_parts(const NormTensor* t, int n, int64_t span, double* part, in
     table.t[i].first_group = (uint32_t)groups;
     groups += cdiv(t[i].n, span);
   }
-  grad_squares_k<<<(unsigned)groups, THREADS, 0, st>>>(table);
+  if (past) grad_squares_k<true><<<(unsigned)groups, THREADS, 0, st>>>(table);
+  else grad_squares_k<false><<<(unsigned)groups, THREADS, 0, st>>>(table);
   *n_parts = (int)groups;
   return hipGetLastError();
 }

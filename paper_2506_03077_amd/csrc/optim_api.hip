@@ -25,6 +25,12 @@ constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 44;
 bool valid_dtype(int dt) { return dt == SBP_F32 || dt == SBP_BF16; }
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+int64_t sum_of(int32_t n, const sbp_adamw_tensor* t) {
+  int64_t s = 0;
+  for (int i = 0; i < n; ++i) s += t[i].n;
+  return s;
+}
+
 int32_t check_table(int32_t n, const sbp_adamw_tensor* t) {
   if (n < 0) return fail(SBP_ERR_SHAPE, "n_tensors must be >= 0");
   if (n > 0 && !t) return fail(SBP_ERR_NULL, "the table of tensors is NULL");
@@ -83,6 +89,7 @@ int32_t streambp_adamw_step(const sbp_adamw_cfg* c, int32_t n_tensors, const sbp
     a.bias1 = (float)(c->lr / -std::expm1(c->step * a.log1));
     a.bias2 = (float)(1.0 / std::sqrt(-std::expm1(c->step * a.log2)));
   }
+  a.past = a.eight && sum_of(n_tensors, tensors) >= OPTIM_PAST;
   AdamwTensor table[ADAMW_TABLE];
   int n = 0;
   int64_t elements = 0;
@@ -115,8 +122,7 @@ int32_t streambp_grad_norm(int32_t n_tensors, const sbp_adamw_tensor* tensors, f
   if (!aligned(norm, 4) || !aligned(grad_scale, 4)) return fail(SBP_ERR_UNSUPPORTED, "norm or grad_scale is not aligned to its elements");
   if (!aligned(workspace, 256)) return fail(SBP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (workspace_bytes < streambp_grad_norm_workspace_bytes(n_tensors)) return fail(SBP_ERR_WORKSPACE, "workspace too small");
-  int64_t total = 0;
-  for (int i = 0; i < n_tensors; ++i) total += tensors[i].n;
+  const int64_t total = sum_of(n_tensors, tensors);
   // (every tensor has at most one span that is not full: no more than NORM_WORKGROUPS + n_tensors of them)
   const int64_t span = std::max<int64_t>(NORM_SPAN, align_up((size_t)cdiv(total, NORM_WORKGROUPS), NORM_SPAN));
   NormTensor table[NORM_TABLE];
@@ -125,7 +131,7 @@ int32_t streambp_grad_norm(int32_t n_tensors, const sbp_adamw_tensor* tensors, f
     if (tensors[i].n > 0) table[n++] = NormTensor{tensors[i].grad, tensors[i].n, 0, tensors[i].grad_dtype};
     if (n == NORM_TABLE || (i == n_tensors - 1 && n > 0)) {
       int more = 0;
-      HIPCHK(norm_parts(table, n, span, (double*)workspace + parts, &more, (hipStream_t)hip_stream));
+      HIPCHK(norm_parts(table, n, span, total >= OPTIM_PAST, (double*)workspace + parts, &more, (hipStream_t)hip_stream));
       parts += more;
       n = 0;
     }

@@ -33,7 +33,7 @@ hipError_t adamw_step(const AdamwArgs& a, const AdamwTensor* t, int n, hipStream
   ++launches;
   return hipSuccess;
 }
-hipError_t norm_parts(const NormTensor* t, int n, int64_t span, double* part, int* n_parts, hipStream_t) {
+hipError_t norm_parts(const NormTensor* t, int n, int64_t span, bool, double* part, int* n_parts, hipStream_t) {
   expect(n >= 1 && n <= NORM_TABLE && span >= NORM_SPAN && span % NORM_SPAN == 0, "a table or span the kernel does not take");
   int64_t groups = 0;
   for (int i = 0; i < n; ++i) { groups += cdiv(t[i].n, span); summed.push_back(t[i]); }
