@@ -261,8 +261,9 @@ typedef struct {
                                     between the sinks and the window may hold anything       */
 } sbp_attn_cfg;
 
-/* What streambp_attn_chunk_backward makes full use of: row statistics, and up to 64 MiB of partial dK/dV where the key
- * blocks alone would leave the chip idle.  A workspace with room for the statistics alone (2 * Hq * c floats, 256-byte
+/* What streambp_attn_chunk_backward makes full use of: row statistics, up to 64 MiB of partial dK/dV where the key
+ * blocks alone would leave the chip idle, and with sinks the parts of their dK/dV (32 MiB, or what the sinks' rows of dk and dv hold if
+ * that is more).  A workspace with room for the statistics alone (2 * Hq * c floats, 256-byte
  * aligned) is accepted too and gives the same results, more slowly where chunks are short: 28 / 4 heads of 128, 512
  * queries from position 0 123 instead of 41 us, from 1792 123 instead of 96, from 2560 on the same. */
 size_t streambp_attn_workspace_bytes(const sbp_attn_cfg *cfg);

@@ -209,9 +209,10 @@ def _ptr(t):
 
 
 def _stream(stream):
+    if stream is not None:
+        return stream.cuda_stream
     torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())      # 2.5 us less than torch.cuda.current_stream(), which makes an object
 
 
 def _workspace(nbytes, device):

@@ -7,7 +7,7 @@ namespace sbp {
 constexpr int ADAMW_BLOCK = 256;                            // elements that share the scale of an 8-bit state
 constexpr int ADAMW_TABLE = 40, NORM_TABLE = 128;           // tensors of a launch: what its arguments hold (less than 4 KB)
 // Elements of a workgroup: one pass, without a loop.  In a loop of passes the loads of one wait for the instructions of the one before: this / a loop over 8192 / over 32768, 545 M weights
-// with 8-bit states 938 / 1038 / 1084 us, 237 M of them in 113 tensors 515 / 563 / 611, 233 M with fp32 states 1338 / 1330 / 1388.
+// with 8-bit states 938 / 1038 / 1084 us, 238 M of them in 111 tensors 515 / 563 / 611, 233 M with fp32 states 1338 / 1330 / 1388.
 constexpr int64_t ADAMW_SPAN = 2048;
 constexpr int64_t ADAMW_MOST = (int64_t)1 << 34;            // ... of a launch: its threads are counted in 32 bits
 constexpr int NORM_WORKGROUPS = 2048;                       // ... of a norm: that many workgroups, and one more per tensor
