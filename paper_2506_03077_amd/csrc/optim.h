@@ -24,12 +24,14 @@ struct AdamwTensor {
   void* param; float* master; void* grad; void *m, *v; uint8_t *m_scale, *v_scale;
   uint32_t first_group;        // workgroups of the tensors before it
   uint32_t index;              // of the call's tensors
+  float keep;                  // 1 - lr weight_decay, without `now`
   int32_t dtype, grad_dtype;
 };
 struct AdamwNow { double lr; int32_t step, pad; };
 struct AdamwArgs {
-  double lr, beta1, beta2, eps;
+  double lr;
   double log1, log2;           // of beta1 and beta2 (-infinity for 0)
+  float beta1, rest1, beta2, rest2, root2, root_rest2, eps;      // 1 - beta1, 1 - beta2, the roots of beta2 and 1 - beta2
   float bias1, bias2;          // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t), without `now`
   uint32_t seed;
   int32_t step;

@@ -3,9 +3,11 @@
 // Both stream memory once: per element AdamW reads weight, gradient and two states and writes weight and states back.  A thread has eight consecutive elements, in
 // 16-byte loads; 32 threads have a block of 256, whose magnitudes meet in registers where the states have 8 bits.
 // What bounds it: memory, with 32-bit states by far.  With 8-bit states and bf16 weights and gradients an element is 10 bytes, in whose time the chip does about 60 vector
-// instructions, so those are counted: 86 in the first form of this kernel, with the library's root and quotient, about 46 now.
-// Measured: 233 M elements with fp32 states and master copies 1335 us, 5.6 TB/s of the bytes above (a large copy runs at 4.8 TB/s); 545 M with 8-bit states 905 us, 6.0 TB/s.
-// The norm reads 933 MB of fp32 gradients in 155 us and 477 MB of bf16 ones in 78 us, 6.0 and 6.1 TB/s.
+// instructions, so those are counted (executed ones, the launch's beginning among them): about 100 in the first form of this kernel, with the library's root and quotient, 4.5 TB/s; 60 with the
+// hardware's and with one product for eight random words; 49.5 with constants folded, what is rare (values not finite, v below the normal range) done again for the wave that has it, and what
+// the host can compute computed there: 545 M elements 910 -> 875 us.
+// Measured: 233 M elements with fp32 states and master copies 1311 us, 5.7 TB/s of the bytes above (a large copy runs at 4.8 TB/s); 545 M with 8-bit states 866 us, 6.3 TB/s.
+// The norm reads 933 MB of fp32 gradients in 155 us and 477 MB of bf16 ones in 75 us, 6.0 and 6.4 TB/s.
 #include "optim.h"
 #include "device.h"
 
@@ -114,6 +116,7 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 // A magnitude as the code of an e4m3 value of 2^(byte - 127): a float 2^120 times smaller than the value has the e4m3 value's exponent, and below its smallest normal
 // one its fixed point, in bits 20 to 26.  u / 2^20 of a step is added before the rest is cut off.
 __device__ __forceinline__ uint32_t e4m3_bits(float x, uint32_t byte) { return __float_as_uint(__builtin_amdgcn_ldexpf(fabsf(x), 7 - (int)byte)); }
+__device__ __forceinline__ uint32_t median(uint32_t a, uint32_t b, uint32_t c) { return max(min(a, b), min(max(a, b), c)); }
 // the top bytes of four words
 __device__ __forceinline__ uint32_t top_bytes(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
   return __builtin_amdgcn_perm(x1, x0, 0x0c0c0703u) | __builtin_amdgcn_perm(x3, x2, 0x07030c0cu);
@@ -125,17 +128,19 @@ __device__ __forceinline__ float root_of(float v) {
   return __builtin_amdgcn_sqrtf(v * (tiny ? 0x1p64f : 1.f)) * (tiny ? 0x1p-32f : 1.f);
 }
 
-struct Consts { float beta1, rest1, beta2, rest2, eps, bias1, bias2; double lr; uint32_t key; float grad_scale; };
+struct Consts { float bias1, bias2, keep; uint32_t key; float grad_scale; };
 
 template <bool WHOLE, typename P, bool MASTER, typename G, bool EIGHT, bool PAST>
-__device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Consts& c, float keep, int64_t e, int n, bool zero) {
-  float g[8], w[8], m[8], v[8];
+__device__ __forceinline__ void eight_elements(const AdamwTensor& t, const AdamwArgs& a, const Consts& c, int64_t e, int n, bool zero) {
+  float g[8], w[8], m[8], v[8], root[8];
   if constexpr (MASTER) get<WHOLE, PAST>(w, t.master + e, n); else get<WHOLE, PAST>(w, (const P*)t.param + e, n);
   get<WHOLE, PAST>(g, (const G*)t.grad + e, n);
   if constexpr (EIGHT) {
     const u32x2 mb = get_bytes<WHOLE, PAST>((const uint8_t*)t.m + e, n), vb = get_bytes<WHOLE, PAST>((const uint8_t*)t.v + e, n);
     const bool in = WHOLE || n > 0;
-    const float ms = in ? scale_of(t.m_scale[e / ADAMW_BLOCK]) : 0.f, vs = in ? scale_of(t.v_scale[e / ADAMW_BLOCK]) : 0.f;
+    // the factors that an element's code and gradient meet, of m and of v's root: products of constants, so that m and v are a product and a sum each
+    const float ms = in ? scale_of(t.m_scale[e / ADAMW_BLOCK]) * a.beta1 : 0.f, vs = in ? scale_of(t.v_scale[e / ADAMW_BLOCK]) * a.root2 : 0.f;
+    const float gm = c.grad_scale * a.rest1, gv = c.grad_scale * a.root_rest2;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const f32x2 m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mb[i], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mb[i], true);
@@ -143,21 +148,32 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
       m[4 * i] = m0[0] * ms; m[4 * i + 1] = m0[1] * ms; m[4 * i + 2] = m1[0] * ms; m[4 * i + 3] = m1[1] * ms;
       v[4 * i] = v0[0] * vs; v[4 * i + 1] = v0[1] * vs; v[4 * i + 2] = v1[0] * vs; v[4 * i + 3] = v1[1] * vs;
     }
+    bool small = false;      // a v below the normal range, which the root's instruction takes for zero
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= v[i];
+    for (int i = 0; i < 8; ++i) {
+      const float y = g[i] * gv;
+      m[i] = fmaf(g[i], gm, m[i]);      // (sums of products are written out: every copy of this code rounds alike)
+      v[i] = fmaf(y, y, v[i] * v[i]);
+      root[i] = __builtin_amdgcn_sqrtf(v[i]);
+      small |= __builtin_amdgcn_classf(v[i], 0x80);
+    }
+    if (__builtin_amdgcn_ballot_w64(small) != 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) root[i] = root_of(v[i]);
+    }
   } else {
     get<WHOLE, PAST>(m, (const float*)t.m + e, n);
     get<WHOLE, PAST>(v, (const float*)t.v + e, n);
-  }
-  float root[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = g[i] * c.grad_scale;
-    m[i] = m[i] * c.beta1 + x * c.rest1;
-    v[i] = v[i] * c.beta2 + x * x * c.rest2;
-    root[i] = root_of(v[i]);
-    w[i] = w[i] * keep - c.bias1 * m[i] * __builtin_amdgcn_rcpf(root[i] * c.bias2 + c.eps);
+    for (int i = 0; i < 8; ++i) {
+      const float x = g[i] * c.grad_scale;
+      m[i] = fmaf(x, a.rest1, m[i] * a.beta1);
+      v[i] = fmaf(x * x, a.rest2, v[i] * a.beta2);
+      root[i] = root_of(v[i]);
+    }
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = fmaf(-(c.bias1 * m[i]), __builtin_amdgcn_rcpf(fmaf(root[i], c.bias2, a.eps)), w[i] * c.keep);
   uint32_t r[8];
   constexpr bool ROUNDS = sizeof(P) == 2 && !MASTER;
   if constexpr (EIGHT || ROUNDS) {
@@ -175,14 +191,15 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = mix_end(r[i]);
   }
+  bool odd = !EIGHT;
   if constexpr (EIGHT) {
     uint32_t mx = 0, vx = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (WHOLE || i < n) { mx = max(mx, __float_as_uint(m[i]) & 0x7fffffffu); vx = max(vx, __float_as_uint(root[i]) & 0x7fffffffu); }
+    for (int i = 0; i < 8; ++i)      // (a root has a sign only as NaN, which is above all others with it too)
+      if (WHOLE || i < n) { mx = max(mx, __float_as_uint(m[i]) & 0x7fffffffu); vx = max(vx, __float_as_uint(root[i])); }
     mx = max_of_block(mx);
     vx = max_of_block(vx);
-    const bool odd = __builtin_amdgcn_ballot_w64(max(mx, vx) >= NOT_FINITE) != 0;      // some element of the wave is not finite: it becomes NaN, and the scale is that of the others
+    odd = __builtin_amdgcn_ballot_w64(max(mx, vx) >= NOT_FINITE) != 0;      // some element of the wave is not finite: it becomes NaN, and the scale is that of the others
     if (odd) {
       mx = vx = 0;
 #pragma unroll
@@ -195,21 +212,22 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
       vx = max_of_block(vx);
     }
     const uint32_t mb = scale_byte(mx), vb = scale_byte(vx);
-    uint32_t a[8], b[8];      // the codes, in the top bytes
+    uint32_t d[8], b[8];      // the codes, in the top bytes
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      a[i] = (((e4m3_bits(m[i], mb) + (r[i] >> 12)) << 4) & 0x7fffffffu) | (__float_as_uint(m[i]) & 0x80000000u);
-      // a root's pattern is zero or more than that of the smallest e4m3 value: code 1 at least
-      b[i] = max(e4m3_bits(root[i], vb) + (r[i] & 0xfffffu), min(__float_as_uint(root[i]), 1u << 20)) << 4;
+      d[i] = (((e4m3_bits(m[i], mb) + (r[i] >> 12)) << 4) & 0x7fffffffu) | (__float_as_uint(m[i]) & 0x80000000u);
+      // A root that is not zero gets code 1 at least.  The median of its code's pattern, 2^20, which is code 1, and its own pattern: zero, or, as a root is 2^-75 or more and a block's byte then
+      // 45 or more, larger than both.
+      b[i] = median(e4m3_bits(root[i], vb) + (r[i] & 0xfffffu), 1u << 20, __float_as_uint(root[i])) << 4;
     }
     if (odd) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if ((__float_as_uint(m[i]) & 0x7fffffffu) >= NOT_FINITE) a[i] = 0x7f000000u;
+        if ((__float_as_uint(m[i]) & 0x7fffffffu) >= NOT_FINITE) d[i] = 0x7f000000u;
         if ((__float_as_uint(root[i]) & 0x7fffffffu) >= NOT_FINITE) b[i] = 0x7f000000u;
       }
     }
-    const u32x2 mc = {top_bytes(a[0], a[1], a[2], a[3]), top_bytes(a[4], a[5], a[6], a[7])}, vc = {top_bytes(b[0], b[1], b[2], b[3]), top_bytes(b[4], b[5], b[6], b[7])};
+    const u32x2 mc = {top_bytes(d[0], d[1], d[2], d[3]), top_bytes(d[4], d[5], d[6], d[7])}, vc = {top_bytes(b[0], b[1], b[2], b[3]), top_bytes(b[4], b[5], b[6], b[7])};
     put_bytes<WHOLE, PAST>((uint8_t*)t.m + e, mc, n);
     put_bytes<WHOLE, PAST>((uint8_t*)t.v + e, vc, n);
     if ((threadIdx.x & 31) == 0 && (WHOLE || n > 0)) { t.m_scale[e / ADAMW_BLOCK] = (uint8_t)mb; t.v_scale[e / ADAMW_BLOCK] = (uint8_t)vb; }
@@ -219,11 +237,16 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
   }
   if constexpr (MASTER) put<WHOLE, PAST>(t.master + e, w, n);
   if constexpr (ROUNDS) {
+    float up[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {      // (then exact; an infinity has nothing below its last bit, NaN stays NaN)
-      const uint32_t b = __float_as_uint(w[i]);
-      w[i] = w[i] != w[i] ? w[i] : __uint_as_float((b + (r[i] & 0xffffu)) & 0xffff0000u);
+    for (int i = 0; i < 8; ++i) up[i] = __uint_as_float((__float_as_uint(w[i]) + (r[i] & 0xffffu)) & 0xffff0000u);      // (then exact; an infinity has nothing below its last bit)
+    // NaN stays NaN: with finite m and root it is the weight's own, or of 0 / 0, and has nothing in its lower half that would carry into the sign
+    if (odd) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) up[i] = w[i] != w[i] ? w[i] : up[i];
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = up[i];
   }
   put<WHOLE, PAST>((P*)t.param + e, w, n);
   if (zero) {
@@ -233,15 +256,14 @@ __device__ __forceinline__ void eight_elements(const AdamwTensor& t, const Const
 }
 
 template <typename P, bool MASTER, typename G, bool EIGHT, bool PAST>
-__device__ __forceinline__ void span_of(const AdamwTensor& t, const Consts& c, int64_t first, bool zero) {
+__device__ __forceinline__ void span_of(const AdamwTensor& t, const AdamwArgs& a, const Consts& c, int64_t first, bool zero) {
   auto whole16 = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
   auto whole8 = [](const void* p) { return ((uintptr_t)p & 7) == 0; };
   const bool aligned = whole16(t.param) && whole16(t.master) && whole16(t.grad) && (EIGHT ? whole8(t.m) && whole8(t.v) : whole16(t.m) && whole16(t.v));
-  const float keep = (float)(1.0 - c.lr * t.weight_decay);
   static_assert(ADAMW_SPAN == TILE, "one pass");
   const int64_t e = first + threadIdx.x * PER;
-  if (aligned && first + TILE <= t.n) eight_elements<true, P, MASTER, G, EIGHT, PAST>(t, c, keep, e, PER, zero);
-  else eight_elements<false, P, MASTER, G, EIGHT, PAST>(t, c, keep, e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)), zero);
+  if (aligned && first + TILE <= t.n) eight_elements<true, P, MASTER, G, EIGHT, PAST>(t, a, c, e, PER, zero);
+  else eight_elements<false, P, MASTER, G, EIGHT, PAST>(t, a, c, e, (int)min((int64_t)PER, max((int64_t)0, t.n - e)), zero);
 }
 
 template <bool EIGHT, bool PAST>
@@ -250,22 +272,22 @@ __global__ __launch_bounds__(THREADS) void adamw_k(const AdamwTable table) {
   const AdamwTensor& t = table.t[tensor_of(table, blockIdx.x)];
   const int64_t first = (int64_t)(blockIdx.x - t.first_group) * ADAMW_SPAN;
   Consts c;
-  c.beta1 = (float)a.beta1; c.rest1 = (float)(1.0 - a.beta1); c.beta2 = (float)a.beta2; c.rest2 = (float)(1.0 - a.beta2);
-  c.eps = (float)a.eps; c.bias1 = a.bias1; c.bias2 = a.bias2; c.lr = a.lr;
+  c.bias1 = a.bias1; c.bias2 = a.bias2; c.keep = t.keep;
   c.grad_scale = a.grad_scale ? *a.grad_scale : 1.f;
   int step = a.step;
   if (a.now) {
     step = max(1, a.now->step);
-    c.lr = a.now->lr;
+    const double lr = a.now->lr;
     __shared__ float bias[2];      // (by one wave: some hundred instructions in fp64)
     if (threadIdx.x < WAVE) {
       const double t1 = -expm1(step * a.log1), t2 = -expm1(step * a.log2);
-      bias[0] = (float)(c.lr / t1);
+      bias[0] = (float)(lr / t1);
       bias[1] = (float)(1.0 / sqrt(t2));
     }
     __syncthreads();
     c.bias1 = bias[0];
     c.bias2 = bias[1];
+    c.keep = (float)(1.0 - lr * t.weight_decay);
   }
   c.key = mix(mix(mix(a.seed) + (uint32_t)step) + t.index);
   const bool zero = a.zero_grads != 0;
@@ -278,9 +300,9 @@ __global__ __launch_bounds__(THREADS) void adamw_k(const AdamwTable table) {
     return;
   }
   const bool gb = t.grad_dtype == DT_BF16;
-  if (t.dtype == DT_F32) { if (gb) span_of<float, false, bf16_t, EIGHT, PAST>(t, c, first, zero); else span_of<float, false, float, EIGHT, PAST>(t, c, first, zero); }
-  else if (t.master) { if (gb) span_of<bf16_t, true, bf16_t, EIGHT, PAST>(t, c, first, zero); else span_of<bf16_t, true, float, EIGHT, PAST>(t, c, first, zero); }
-  else { if (gb) span_of<bf16_t, false, bf16_t, EIGHT, PAST>(t, c, first, zero); else span_of<bf16_t, false, float, EIGHT, PAST>(t, c, first, zero); }
+  if (t.dtype == DT_F32) { if (gb) span_of<float, false, bf16_t, EIGHT, PAST>(t, a, c, first, zero); else span_of<float, false, float, EIGHT, PAST>(t, a, c, first, zero); }
+  else if (t.master) { if (gb) span_of<bf16_t, true, bf16_t, EIGHT, PAST>(t, a, c, first, zero); else span_of<bf16_t, true, float, EIGHT, PAST>(t, a, c, first, zero); }
+  else { if (gb) span_of<bf16_t, false, bf16_t, EIGHT, PAST>(t, a, c, first, zero); else span_of<bf16_t, false, float, EIGHT, PAST>(t, a, c, first, zero); }
 }
 
 hipError_t adamw_step(const AdamwArgs& a, const AdamwTensor* t, int n, hipStream_t st) {

@@ -80,7 +80,9 @@ int32_t streambp_adamw_step(const sbp_adamw_cfg* c, int32_t n_tensors, const sbp
   if (int32_t rc = check_adamw(c, n_tensors, tensors, now != nullptr)) return rc;
   if (!aligned(grad_scale, 4) || !aligned(now, 8)) return fail(SBP_ERR_UNSUPPORTED, "grad_scale or now is not aligned to its elements");
   AdamwArgs a{};
-  a.lr = c->lr; a.beta1 = c->beta1; a.beta2 = c->beta2; a.eps = c->eps;
+  a.lr = c->lr; a.eps = (float)c->eps;
+  a.beta1 = (float)c->beta1; a.rest1 = (float)(1.0 - c->beta1);
+  a.beta2 = (float)c->beta2; a.rest2 = (float)(1.0 - c->beta2); a.root2 = (float)std::sqrt(c->beta2); a.root_rest2 = (float)std::sqrt(1.0 - c->beta2);
   a.seed = c->seed; a.step = c->step; a.grad_scale = grad_scale; a.now = (const AdamwNow*)now;
   a.eight = c->state == SBP_STATE_8BIT; a.zero_grads = c->zero_grads;
   a.log1 = std::log(c->beta1); a.log2 = std::log(c->beta2);
@@ -103,7 +105,7 @@ int32_t streambp_adamw_step(const sbp_adamw_cfg* c, int32_t n_tensors, const sbp
     const sbp_adamw_tensor& x = tensors[i];
     if (x.n == 0) continue;
     if (n == ADAMW_TABLE || elements + x.n > ADAMW_MOST) HIPCHK(flush());
-    table[n++] = AdamwTensor{x.n, x.weight_decay, x.param, x.master, x.grad, x.m, x.v, (uint8_t*)x.m_scale, (uint8_t*)x.v_scale, 0, (uint32_t)i, x.dtype, x.grad_dtype};
+    table[n++] = AdamwTensor{x.n, x.weight_decay, x.param, x.master, x.grad, x.m, x.v, (uint8_t*)x.m_scale, (uint8_t*)x.v_scale, 0, (uint32_t)i, (float)(1.0 - c->lr * x.weight_decay), x.dtype, x.grad_dtype};
     elements += x.n;
   }
   HIPCHK(flush());

@@ -3,7 +3,7 @@
 
 Bounds, eps = 2^-24 (half a step of fp32, relative): constants are rounded once, products and sums once each.
   m: two products of three roundings (constant, scaled gradient, product) and a sum: 4 eps (|b1 m| + |(1 - b1) g|), tested with 6
-  v: gradient scaled, squared, times a rounded constant, and a sum: at most 6 eps of v, tested with 8
+  v: gradient scaled, squared, times a rounded constant, and a sum: at most 6 eps of v (8-bit states: times a constant of three roundings' product, squared, and a sum: 7), tested with 8
   p: m's error and at most 12 roundings of the update (v's 8 count half through the root; root, two products, sum, quotient, constant, product), the decayed weight's three and
      the difference: bias1 / den * 6 eps Sm + 12 eps |update| + 4 eps |p|, tested with 16 and 6
 """
