@@ -236,9 +236,10 @@ __device__ __forceinline__ void query_tile_of(int id, int n_qt, int heads, int& 
 template <bool SINKS, int NK>
 struct KeyTiles {
   int kt0, n_window, sink0 = 0, n_sink = 0, kv_first, sink_end;      // keys kv_first .. sink_end - 1 are the sinks
-  __device__ __forceinline__ KeyTiles(int first, int sinks, int first_tile, int n_tiles, int n_total)
+  __device__ __forceinline__ KeyTiles(int first, int sinks, int first_tile, int n_tiles, int n_keys, int n_total)
       : kt0(first_tile), n_window(max(0, n_tiles - first_tile)), kv_first(first), sink_end(first + min(sinks, max(0, n_total - first))) {
     if constexpr (SINKS) {
+      if (first >= n_keys) n_window = 0;      // padding up to its last query: there is no row to read
       sink0 = first / NK;
       n_sink = max(0, min(min((sink_end + NK - 1) / NK, kt0), n_tiles) - sink0);
     }
@@ -325,7 +326,7 @@ __device__ __forceinline__ void fwd_tile(bf16_t* q, const bf16_t* __restrict__ k
   const int wave_lo_min = first_key(wave_first_qpos);                 // lowest first key in the wave (its first query)
   const int wave_lo_max = first_key(wave_last_key);                   // highest one (its last query)
   const int kt0 = first_key(q_start + q0) / TK;                       // first key tile any query of the workgroup sees (SINKS: in its window)
-  const KeyTiles<SINKS, TK> tiles(kv_first, sinks, kt0, n_tiles, n_total);
+  const KeyTiles<SINKS, TK> tiles(kv_first, sinks, kt0, n_tiles, n_keys, n_total);
   const int n_it = SPLIT ? (tiles.n() + 1) / 2 : tiles.n();
   auto tile_of = [&](int i) { return tiles.at(SPLIT ? 2 * i + grp : i); };
 
@@ -763,7 +764,7 @@ __device__ __forceinline__ void dq_tile(DqShared<DH, SPLIT>& sh, int q_block, in
   auto first_key = [&](int p) { return max(kv_first, window > 0 ? p - window + 1 : 0); };   // left edge of the visible range
   const int wave_lo_min = first_key(wave_first_qpos), wave_lo_max = first_key(wave_last_key);
   const int kt0 = first_key(q_start + q0) / NK;
-  const KeyTiles<SINKS, NK> tiles(kv_first, sinks, kt0, n_tiles, n_total);
+  const KeyTiles<SINKS, NK> tiles(kv_first, sinks, kt0, n_tiles, n_keys, n_total);
   // tile i of this wave's sequence
   auto tile_of = [&](int i) { return tiles.at(SPLIT ? 2 * i + grp : i); };
   const int n_it = SPLIT ? (tiles.n() + 1) / 2 : tiles.n();
@@ -1230,7 +1231,7 @@ __device__ __forceinline__ void dkv_block(DkvShared<DH>& sh, int key_block, int 
   int n_qt = (c + QT - 1) / QT;
   if (SINKS) n_qt = min(n_qt, max(0, key0 + KV_TILE - 2 + (reach - q_start)) / QT + 1);
   else if (window > 0) n_qt = min(n_qt, max(0, key0 + KV_TILE - 1 + window - 1 - q_start) / QT + 1);
-  const int n_all = key0 + KV_TILE <= kv_first || (SINKS && key0 >= key_end) ? 0 : max(0, n_qt - qt_first) * G;      // (a sequence of several may hide blocks that others see)
+  const int n_all = key0 + KV_TILE <= kv_first || (SINKS && max(key0, kv_first) >= key_end) ? 0 : max(0, n_qt - qt_first) * G;      // (a sequence of several may hide blocks that others see)
   auto share = [&](int z) { return (int)((int64_t)n_all * z / slices); };      // first step of share z
   for (int z = part ? slice : 0, z_last = IN_TURN ? 0 : part ? slice : slices - 1; z <= z_last; ++z) {
   const int it0 = IN_TURN ? 0 : share(z), n_iter = (IN_TURN ? n_all : share(z + 1)) - it0;

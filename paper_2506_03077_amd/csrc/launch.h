@@ -179,7 +179,7 @@ struct AttnArgs {
   float scale;
   int window = 0;          // > 0: a query at position t sees only keys t - window < u <= t; at most all keys (attn_set_window)
   int kv_first = 0;        // key positions before this one are padding: never visible
-  int sinks = 0;           // the first `sinks` keys from kv_first on stay visible to every later query; 0 without a window, at most all keys (attn_set_window)
+  int sinks = 0;           // the first `sinks` keys from kv_first on stay visible to every later query; 0 without a window, at most all keys, or one (attn_set_window)
   // Several sequences in one call, up to ATTN_MAX_SEQS: `batch` of q_len queries and keys each, one behind the other (q_start = 0; lse [batch, Hq, c],
   // delta [batch, 2, Hq, c]), kv_firsts their kv_first on the host (or NULL: kv_first for all; else kv_first is the least of them).
   int batch = 1;
@@ -265,8 +265,11 @@ inline int attn_sink_slices(const AttnArgs& a, size_t max_bytes) {
 }
 // What a caller's window and sinks come to: no more than all keys (positions plus a window are 32-bit sums in the kernels)
 inline void attn_set_window(AttnArgs& a, int window, int sinks) {
-  a.window = std::min(window, a.q_start + a.q_len);
-  a.sinks = a.window > 0 ? (int)std::min<int64_t>(sinks, std::max<int64_t>(0, (int64_t)a.q_start + a.q_len - a.kv_first)) : 0;
+  const int n = a.q_start + a.q_len;
+  a.window = std::min(window, n);
+  // (one at least: rows that no query sees are left alone by the kernels with sinks)
+  a.sinks = a.window > 0 ? std::min(sinks, std::max(1, n - std::min(n, a.kv_first))) : 0;
+  if (a.sinks > 0) a.kv_first = std::min(a.kv_first, n);
 }
 
 // ---- LM head rows ----

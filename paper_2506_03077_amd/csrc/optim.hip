@@ -3,7 +3,7 @@
 // Both stream memory once: per element AdamW reads weight, gradient and two states and writes weight and states back.  A thread has eight consecutive elements, in
 // 16-byte loads; 32 threads have a block of 256, whose magnitudes meet in registers where the states have 8 bits.
 // What bounds it: memory, with 32-bit states by far.  With 8-bit states and bf16 weights and gradients an element is 10 bytes, in whose time the chip does about 60 vector
-// instructions, so those are counted (executed ones, the launch's beginning among them): about 100 in the first form of this kernel, with the library's root and quotient, 4.5 TB/s; 60 with the
+// instructions, so those are counted (executed ones, the launch's beginning among them): by its code 86 an element in the first form of this kernel, with the library's root and quotient, 4.5 TB/s; 60 with the
 // hardware's and with one product for eight random words; 49.5 with constants folded, what is rare (values not finite, v below the normal range) done again for the wave that has it, and what
 // the host can compute computed there: 545 M elements 910 -> 875 us.
 // Measured: 233 M elements with fp32 states and master copies 1311 us, 5.7 TB/s of the bytes above (a large copy runs at 4.8 TB/s); 545 M with 8-bit states 866 us, 6.3 TB/s.

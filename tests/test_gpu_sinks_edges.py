@@ -102,3 +102,18 @@ def test_two_streams_at_once():
         torch.cuda.synchronize()
         for x, (_, _, want) in zip(got, cases):
             assert all(torch.equal(a, b) for a, b in zip(x, want))
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("f32", 16)])
+@pytest.mark.parametrize("s,c,kv_first", [(0, 2, 2), (0, 1, 5), (200, 77, 277), (200, 77, 1000), (200, 77, MOST), (100, 300, 400)])
+def test_padding_all_the_way(dtype, dh, s, c, kv_first):
+    """No query sees anything: the outputs say so, and dk and dv keep their bits, whatever K and V hold."""
+    inp = synth.attn_inputs(4, 2, dh, s, c, dtype, 9)
+    q, d_o = dev(inp["q"], dtype), dev(inp["d_o"], dtype)
+    k = torch.full((s + c, 2, dh), float("nan") if dtype == "bf16" else 1.0, dtype=tdtype(dtype), device="cuda")
+    ac = sb.attn_cfg(code(dtype), 4, 2, dh, s, c, 0.1, window=64, kv_first=kv_first, sinks=3)
+    o, lse = sb.streambp_attn_chunk_forward(ac, q, k, k)
+    start = [torch.randn((s + c, 2, dh), device="cuda") for _ in range(2)]
+    dq, dk, dv = sb.streambp_attn_chunk_backward(ac, q, k, k, o, lse, d_o, dk=start[0].clone(), dv=start[1].clone())
+    assert not bool(o.any()) and bool((lse == -float("inf")).all()) and not bool(dq.any())
+    assert torch.equal(dk, start[0]) and torch.equal(dv, start[1])
