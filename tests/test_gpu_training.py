@@ -85,3 +85,74 @@ def test_steps(name, grad_dtype, state, master):
                 assert not bool(x["grad"].any()), "a gradient was not cleared"
             losses.append(want_loss)
     assert len(set(losses)) == 3                                                  # each step used the weights that the one before left
+
+
+def now_of(lr, step):
+    raw = np.zeros(16, np.uint8)
+    raw[:8] = np.frombuffer(np.float64(lr).tobytes(), np.uint8)
+    raw[8:12] = np.frombuffer(np.int32(step).tobytes(), np.uint8)
+    return torch.from_numpy(raw).cuda()
+
+
+def test_a_captured_training_step():
+    """The whole step in one graph, replayed with other tokens, rates and step numbers: the bits of the same step taken eagerly, weights and 8-bit states among them."""
+    cfg = dict(dtype="bf16", hidden=256, n_q_heads=4, n_kv_heads=2, head_dim=128, mlp_width=512, vocab=150)
+    L, T, d = 2, 300, 256
+    lc = sb.layer_cfg(sb.SBP_BF16, 1, T, 96, d, 4, 2, 128, 512, window=WINDOW, sinks=SINKS)
+    sc = sb.stack_cfg(lc, L, 150, 100, sb.SBP_OBJ_SFT, 1.0 / T)
+    ids, targets = (torch.zeros((1, T), dtype=torch.int32, device="cuda") for _ in range(2))
+    now, norm, factor = now_of(1e-3, 1), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    ws = torch.empty(sb.streambp_stack_workspace_bytes(sc), dtype=torch.uint8, device="cuda")
+    acfg = sb.adamw_cfg(**HYPER, step=1, state=sb.SBP_STATE_8BIT, seed=SEED, zero_grads=True)
+
+    def model():
+        layers = [{n: dev(v, "bf16") for n, v in synth.layer_weights(cfg, seed=10 + l).items()} for l in range(L)]
+        rng = np.random.default_rng(5)
+        rest = [dev(1 + rng.normal(0, 0.02, d), "bf16"), dev(rng.normal(0, 0.05, (150, d)), "bf16"), dev(rng.normal(0, 1, (150, d)), "bf16")]
+        grads = dict(dlayers=[sb.new_layer_grads(w) for w in layers], dg_final=torch.zeros(d, device="cuda"), dw_head=torch.zeros((150, d), device="cuda"),
+                     demb=torch.zeros((150, d), device="cuda"), dx0=torch.empty((1, T, d), dtype=torch.bfloat16, device="cuda"), loss=torch.zeros(1, device="cuda"),
+                     n_active=torch.zeros(1, dtype=torch.int64, device="cuda"))
+        pairs = [(w[n], g[n]) for w, g in zip(layers, grads["dlayers"]) for n in sb.WEIGHT_NAMES] + list(zip(rest, (grads["dg_final"], grads["dw_head"], grads["demb"])))
+        table = sb.adamw_tensors([dict(sb.new_adamw_states(p, sb.SBP_STATE_8BIT), grad=g, weight_decay=0.1) for p, g in pairs])
+        ckpt = [torch.empty((1, T, d), dtype=torch.bfloat16, device="cuda") for _ in range(L + 1)]
+        norm_ws = torch.empty(sb.streambp_grad_norm_workspace_bytes(len(table)), dtype=torch.uint8, device="cuda")
+
+        def step():
+            sb.streambp_stack_forward(sc, layers, ckpt, rest[2], ids, workspace=ws)
+            sb.streambp_stack_backward(sc, layers, rest[0], rest[1], ckpt, targets, ids=ids, workspace=ws, **grads)
+            sb.streambp_grad_norm(table, 0.05, norm, factor, norm_ws)
+            sb.streambp_adamw_step(acfg, table, grad_scale=factor, now=now)
+        return step, table, grads
+
+    step, table, grads = model()
+    eager, other, eager_grads = model()
+    kept = [{n: x.clone() for n, x in t.items() if n != "weight_decay"} for t in table.tensors]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    torch.cuda.synchronize()
+    for t, k in zip(table.tensors, kept):
+        for n in k:
+            t[n].copy_(k[n])
+    for i in range(1, 5):
+        gen = torch.Generator("cuda").manual_seed(i)
+        ids.copy_(torch.randint(0, 150, (1, T), generator=gen, device="cuda", dtype=torch.int32))
+        targets.copy_(torch.randint(0, 150, (1, T), generator=gen, device="cuda", dtype=torch.int32))
+        now.copy_(now_of(HYPER["lr"] / i, i))
+        for g in (grads, eager_grads):
+            g["loss"].zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = (norm.clone(), factor.clone(), grads["loss"].clone(), grads["dx0"].clone())
+        eager()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (norm, factor, eager_grads["loss"], eager_grads["dx0"])))
+        for t, o in zip(table.tensors, other.tensors):
+            for n in kept[0]:
+                assert torch.equal(t[n].reshape(-1).view(torch.uint8), o[n].reshape(-1).view(torch.uint8)), (i, n)
