@@ -46,3 +46,28 @@ def test_norm(dtype):
     norm, factor = sb.streambp_grad_norm(sb.adamw_tensors([dict(grad=g) for g in grads]), want / 2)
     # squares and sums of eight in fp32, half of their relative error through the root, and the result's rounding; the factor three roundings more
     assert abs(norm.item() - want) <= 5 * 2.0 ** -24 * want and abs(factor.item() - 0.5) <= 8 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("eight", [True, False])
+def test_elements_past_32_bits(eight, monkeypatch):
+    """A bf16 tensor of more than 2^32 elements: its last ones are found, and have random words of their own (the high half of the index is part of the key)."""
+    first, n = 2 ** 32 + 512, 2 ** 32 + 512 + 5000
+    if torch.cuda.mem_get_info()[0] < 64e9:
+        pytest.skip("26 GB, 52 with 32-bit states")
+    small, _ = make(5000, torch.bfloat16, torch.bfloat16, False, eight, 7)
+    old = before(small, eight)
+    t = dict(param=torch.zeros(n, dtype=torch.bfloat16, device="cuda"), grad=torch.zeros(n, dtype=torch.bfloat16, device="cuda"))
+    t.update({k: v for k, v in sb.new_adamw_states(t["param"], int(eight)).items() if k != "param"})
+    for k in t:
+        at = first // 256 if k.endswith("scale") else first
+        t[k][at:at + len(small[k])].view(torch.uint8).copy_(small[k].view(torch.uint8))
+    norm, _ = sb.streambp_grad_norm(sb.adamw_tensors([dict(grad=t["grad"])]))
+    want = float(small["grad"].double().norm())
+    assert abs(norm.item() - want) <= 5 * 2.0 ** -24 * want
+    sb.streambp_adamw_step(sb.adamw_cfg(**HYPER, step=3, seed=11, state=int(eight)), sb.adamw_tensors([dict(t, weight_decay=0.1)]))
+    torch.cuda.synchronize()
+    words = optim.random_bits
+    monkeypatch.setattr(optim, "random_bits", lambda seed, step, tensor, k: words(seed, step, tensor, k, first=first))
+    last = {k: (x[first // 256:] if k.endswith("scale") else x[first:]).clone() for k, x in t.items()}
+    check(last, old, 0, 3, eight, 0.1, seed=11)
+    assert not any(bool(x.any()) for x in t["param"][:first].split(2 ** 28))
