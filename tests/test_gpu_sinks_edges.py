@@ -117,3 +117,30 @@ def test_padding_all_the_way(dtype, dh, s, c, kv_first):
     dq, dk, dv = sb.streambp_attn_chunk_backward(ac, q, k, k, o, lse, d_o, dk=start[0].clone(), dv=start[1].clone())
     assert not bool(o.any()) and bool((lse == -float("inf")).all()) and not bool(dq.any())
     assert torch.equal(dk, start[0]) and torch.equal(dv, start[1])
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 8, 4, 128), ("bf16", 8, 8, 64), ("f32", 4, 4, 64)])
+def test_a_cache_of_more_than_4_GiB(dtype, hq, hkv, dh):
+    """Sinks at its beginning, a window at its end, nothing between them is looked at (bf16: NaN)."""
+    if torch.cuda.mem_get_info()[0] < 64e9:
+        pytest.skip("27 GB")
+    s, c, window, sinks = 4_400_000, 333, 200, 5
+    n, lo = s + c, s - window - 50
+    gap = lo - sinks                                  # rows that the oracle is spared: its row u + sinks is row lo + u
+    inp = synth.attn_inputs(hq, hkv, dh, s - gap, c, dtype, 11)
+    k, v = (torch.full((n, hkv, dh), float("nan") if dtype == "bf16" else 1.0, dtype=tdtype(dtype), device="cuda") for _ in range(2))
+    assert k.numel() * k.element_size() > 2 ** 32
+    for x, name in ((k, "k"), (v, "v")):
+        x[:sinks], x[lo:] = dev(inp[name][:sinks], dtype), dev(inp[name][sinks:], dtype)
+    q, d_o = dev(inp["q"], dtype), dev(inp["d_o"], dtype)
+    ac = sb.attn_cfg(code(dtype), hq, hkv, dh, s, c, dh ** -0.5, window, 0, sinks)
+    o, lse, dq, dk, dv = run(ac, q, k, v, d_o)
+    torch.cuda.synchronize()
+    assert not any(bool(x[sinks:lo].any()) for x in (dk, dv))
+    o_ref, lse_ref = o_attn.chunk_forward(inp["q"], inp["k"], inp["v"], s - gap, dh ** -0.5, window, 0, sinks)
+    refs = o_attn.chunk_backward(inp["q"], inp["k"], inp["v"], inp["d_o"], s - gap, dh ** -0.5, window, 0, sinks)
+    assert_close(host(o), o_ref, TOL[dtype], "o")
+    assert np.abs(host(lse) - lse_ref).max() < 1e-5
+    assert_close(host(dq), refs[0], TOL[dtype], "dq")
+    for x, ref, name in ((dk, refs[1], "dk"), (dv, refs[2], "dv")):
+        assert_close(np.concatenate([host(x[:sinks]), host(x[lo:])]), ref, TOL[dtype], name)
